@@ -56,7 +56,7 @@ enum {
   MOE_ERR_HIP = 4          /* a launch failed; see moe_last_error()                          */
 };
 
-enum { MOE_F32 = 0, MOE_BF16 = 1 };
+enum { MOE_F32 = 0, MOE_BF16 = 1, MOE_MX8 = 2 /* of a key/value cache only */ };
 
 /* Library version, "major.minor.patch" ([host] static string). */
 const char* moe_version(void);
@@ -289,6 +289,85 @@ size_t moe_router_bwd_workspace_bytes(int dtype, int T, int d, int E);
 int32_t moe_router_bwd(const float* dlogits, const void* x, const void* w_router, int dtype,
                        int T, int d, int E, int accumulate, void* dx, void* dw_router,
                        void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Rotary positions (RoPE is one of the efficient kernels of Sec. 3.2.5; the paper gives no formula).
+ *   Head element pairs (a, b) = (i, i + rot/2), or (2i, 2i + 1) when interleaved != 0, i < rot/2, become
+ *     a' = a c - b s,  b' = b c + a s,   c = cos[positions[t], i],  s = sin[positions[t], i];
+ *   elements rot .. D - 1 are copied.  fp32 arithmetic, one rounding to the element type.
+ *   moe_rope_bwd turns the gradients of the outputs back: s becomes -s, nothing else changes.
+ *   q [T, Hq, D] and k [T, Hk, D] of element type dtype, with any strides (in elements) between tokens and heads that
+ *   are multiples of 16 bytes, a head's elements being contiguous; outputs alike.  q_out may be q, and k_out k, with the
+ *   same strides; other overlaps are not allowed.  Either of q and k may be left out (null, its number of heads 0).
+ *   positions [T] i32; cos, sin [n_pos, rot/2] f32.  Positions outside [0, n_pos) are taken as the nearest that is inside.
+ *   D a multiple of 8 up to 512, rot a multiple of 16 up to D; rot == 0 copies and needs no table.  T == 0 is a no-op.
+ *
+ * moe_rope_table: cos[p, i] = amplitude cos(p freq[i]), sin alike, p < n_pos, i < half; freq [half] f64 (device).  The angle is
+ *   formed, reduced and evaluated in 64 bits and the result rounded once, so the last positions of a long context are as exact as the first.
+ *   Scaled contexts are a matter of freq and amplitude.
+ */
+int32_t moe_rope_table(const double* freq, int n_pos, int half, double amplitude, float* cos, float* sin, void* stream);
+int32_t moe_rope_fwd(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k, int64_t k_stride_t,
+                     int64_t k_stride_h, int dtype, int T, int Hq, int Hk, int D, int rot, const int32_t* positions,
+                     const float* cos, const float* sin, int n_pos, int interleaved, void* q_out, int64_t qo_stride_t,
+                     int64_t qo_stride_h, void* k_out, int64_t ko_stride_t, int64_t ko_stride_h, void* stream);
+int32_t moe_rope_bwd(const void* dq, int64_t q_stride_t, int64_t q_stride_h, const void* dk, int64_t k_stride_t,
+                     int64_t k_stride_h, int dtype, int T, int Hq, int Hk, int D, int rot, const int32_t* positions,
+                     const float* cos, const float* sin, int n_pos, int interleaved, void* dq_in, int64_t qo_stride_t,
+                     int64_t qo_stride_h, void* dk_in, int64_t ko_stride_t, int64_t ko_stride_h, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Paged key/value cache for generation (a widening beyond the paper, which trains).
+ * A page holds page_size consecutive tokens of one sequence, for all key/value heads:
+ *   k, v [pages, heads, page_size, dim] of dtype MOE_F32 or MOE_BF16, or MOE_MX8: E4M3 codes (one byte an element) with
+ *   k_scales, v_scales [pages, heads, page_size, dim/32] u8, value = 2^(scale - 127) * code, blocks and rounding as in moe_mx8_quantise.
+ *   page_stride, scale_page_stride: elements (bytes for the scales) from one page to the next; within a page all is dense.
+ *   page_size a power of two from 16 to 4096; dim 64, 128, 192 or 256.
+ * The descriptor is read on the host during a call [host]; its pointers are device pointers.
+ * Token t of a sequence lies in page block_table[b, t / page_size] at place t % page_size; its slot is page * page_size + place.
+ * Activations beside the cache are f32 for an MOE_F32 cache and bf16 for the other two.
+ */
+typedef struct {
+  int32_t dtype, pages, heads, page_size, dim, reserved;
+  void *k, *v, *k_scales, *v_scales;
+  int64_t page_stride, scale_page_stride;
+} moe_kv_cache_t;
+
+/* New keys and values into the cache, the keys rotated on the way as by moe_rope_fwd (rot == 0: stored as they are), and the queries of
+ * the same tokens rotated into q_out in the same launch (Hq == 0: no queries).
+ *   k, v [T, heads, dim], q [T, Hq, dim], q_out alike: strides as in moe_rope_fwd; q_out may be q with the same strides.
+ *   slots [T] i64: a negative one, or one beyond the cache, leaves the token out of the cache (its query is still rotated).
+ *   Slots of one call are distinct.  For MOE_MX8 rotated keys are quantised straight from fp32; NaN and infinities are not supported there.
+ */
+int32_t moe_kv_cache_write(const moe_kv_cache_t* cache, const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v,
+                           int64_t v_stride_t, int64_t v_stride_h, int T, const int64_t* slots, const void* q,
+                           int64_t q_stride_t, int64_t q_stride_h, int Hq, int rot, const int32_t* positions,
+                           const float* cos, const float* sin, int n_pos, int interleaved, void* q_out,
+                           int64_t qo_stride_t, int64_t qo_stride_h, void* stream);
+
+/* Cached keys and values back into packed rows: row r in [row_start[b], row_start[b+1]) is token first[b] + r - row_start[b]
+ * of sequence b (first == NULL: from its first token on).
+ *   block_table [B, max_pages] i32; row_start [B+1] i32, ascending; first [B] i32 or NULL;
+ *   k_out, v_out [rows, heads, dim] f32 (MOE_F32) or bf16, dense.  An MOE_MX8 value is exact in bf16 down to bf16's smallest numbers.
+ *   Rows at or beyond row_start[B] are left alone; tokens beyond the page table and pages outside the cache read as zeros.
+ */
+int32_t moe_kv_cache_read(const moe_kv_cache_t* cache, const int32_t* block_table, int max_pages, const int32_t* row_start,
+                          const int32_t* first, int B, int rows, void* k_out, void* v_out, void* stream);
+
+/* Attention of one new token per sequence over the cache.
+ *   out[b, h, :] = sum_t p_t v_t,  p = softmax over t of scale <q[b, h, :], k_t>,  key/value head h / (Hq / heads),
+ *   t from max(0, len - window) (window == 0: from 0) to len - 1, len = lens[b] (taken as at most max_pages * page_size).
+ *   q [B, Hq, dim] (strides q_stride_b, q_stride_h, multiples of 16 bytes), out [B, Hq, dim] dense, both f32 for an MOE_F32 cache, else bf16;
+ *   lse [B, Hq] f32 or NULL: the natural logarithm of the sum of exp(score), with which results over parts of a context are joined.
+ *   A sequence without tokens gets zeros and lse = -inf.  Places of the cache outside a sequence's tokens may hold anything.
+ *   Scores, softmax and sums are fp32; the result is rounded once.  Page ids are taken as the nearest that exists.
+ *   The order of the sums depends on lens, B and the sizes only: the same call gives the same bits.
+ *   Hq a multiple of heads; B * heads * context length up to 2^31 or so (MOE_ERR_UNSUPPORTED beyond).
+ */
+size_t moe_paged_attn_decode_workspace_bytes(int B, int Hq, int heads, int dim, int page_size, int max_pages);
+int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int64_t q_stride_h, const moe_kv_cache_t* cache,
+                              const int32_t* block_table, int max_pages, const int32_t* lens, int B, int Hq, float scale,
+                              int window, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * Launch hook for measurement and tracing harnesses (not part of the layer's arithmetic; the

@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmoe_gfx950.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
-SOURCES = ["api.hip", "route.hip", "permute.hip", "gemm_f32.hip", "gemm_bf16.hip"]
+SOURCES = ["api.hip", "route.hip", "permute.hip", "gemm_f32.hip", "gemm_bf16.hip", "rope.hip", "attn_decode.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

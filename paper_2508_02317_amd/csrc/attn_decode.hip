@@ -1,0 +1,621 @@
+// Attention of one new token per sequence over a paged key/value cache, split over the contexts' length and joined.
+//
+//     out[b, h] = sum_t p_t v_t / sum_t p_t,   p_t = exp(scale <q[b, h], k_t> - m),   m = max_t scale <q[b, h], k_t>
+//
+// All heads of a group share their keys and values, so an element of the cache is read once and used for the whole group: 2 * 16 operations
+// per byte at most (bf16, 16 heads), far below what the matrix units need to be busy.  The kernel is bound by the rate at which the cache
+// arrives, and its layout serves that rate:
+//
+//   * No key or value passes through LDS.  A wave takes kSub tokens at a time, and the operands of the matrix instructions are what its lanes
+//     load, 16 bytes each.  With lane = 16 c + n:
+//       scores   S^T = K Q^T   row = token 16 a + n of the wave's tokens (a = 0, 1), column = head n, reduction along the head's elements
+//                              in any order that keys and queries share: a lane reads 16 bytes of its token's row
+//       result   lane holds the scores of head n and the tokens 16 a + 4 c + r (r = 0..3)
+//       output   O^T = V^T P^T row = element, column = head n, reduction along tokens, in any order that values and p share: the order in
+//                              which the scores lie already, so p goes from one product to the next without leaving its lane.  A
+//                              lane reads the elements [n * kE, + kE) of the tokens 16 a + 4 c + r, whole rows of memory per 16 lanes, and one byte
+//                              permutation per pair of tokens makes the operand
+//     A head's scores, maximum, sum and output elements are all in the lanes of the same n: the running rescaling is lane-local.
+//   * The loads of the next tokens are in flight while these are worked on: keys from the moment the scores are formed, values from the moment
+//     the output is.  Every byte offset of a lane is the same for all tokens; pages enter as scalar bases.
+//   * The tokens of all sequences and heads form one line of tiles of 4 kSub tokens, cut into equal pieces, one per workgroup: lengths may
+//     differ as they like.  A workgroup that does not see the whole context of a head leaves its maximum, sum and unscaled output behind, at most
+//     two of them, and a second launch joins those.  The cut depends on lens alone, so results do not change from call to call.
+//
+// Scores are fp32 sums of exact products (8-bit values are exact in bf16).  p is split into two bf16 numbers, together exact to 2^-16, so that
+// rounding it leaves the result as if it had not been rounded: one bf16 alone made the error of the output 1.4 times that of its own rounding,
+// and the second product costs nothing while bytes are awaited.
+#include <cmath>
+#include <type_traits>
+#include "attn_plan.h"
+#include "launch_plan.h"
+#include "moe_common.h"
+
+namespace moe {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+struct Args {
+  const void* q;
+  int64_t q_stride_b, q_stride_h;
+  const char *k, *v, *ks, *vs;
+  int64_t page_bytes, scale_page_bytes;               // from one page to the next
+  int pages, page_shift;
+  const int32_t *block_table, *lens;
+  int max_pages, B, Hq, Hkv, group, parts, heads;      // group: query heads per key head, in `parts` units of up to `heads`
+  float scale_log2;
+  int window;
+  void* out;
+  float* lse;
+  int32_t* unit_pieces;                                // [B * Hkv * parts][2]: first workgroup (its slot in bit 0) and last of a cut unit, or -1
+  float* slots;                                        // [2 W][heads][D + 2]: maximum, sum, output
+};
+
+__device__ __forceinline__ float row_max4(float v) {   // over the four lanes of the same n
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_sum4(float v) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float scale_of(uint32_t code) {   // 2^(code - 127)
+  return __uint_as_float(code << 23);
+}
+// Words loaded from memory with the alignment that head rows have: whole vectors of 4, 2 or 1 words.
+template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const char* p) {
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
+    }
+  } else if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const u32x2 x = reinterpret_cast<const u32x2*>(p)[i];
+      w[2 * i] = x[0]; w[2 * i + 1] = x[1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+  }
+}
+
+// What a wave holds of its tokens, and the products with it.
+template <int KIND, int D> struct Wave {
+  static constexpr bool kF32 = KIND == MOE_F32, kMx = KIND == MOE_MX8;
+  static constexpr int kHalves = kF32 ? 1 : 2, kSub = 16 * kHalves, kTile = kWaves * kSub;
+  static constexpr int kG = D % 128 == 0 ? 128 : 64, kE = kG / 16, kNG = D / kG;   // a lane's values: kE elements of each of kNG groups of kG
+  static constexpr int kEs = kF32 ? 4 : kMx ? 1 : 2, kRow = D * kEs;               // bytes of an element, of a token's row
+  static constexpr int kKPieces = kMx ? D / 64 : kF32 ? D / 16 : D / 32;           // 16-byte pieces of a key row that a lane reads
+  static constexpr int kKStep = kMx ? 64 : kF32 ? 64 : 64;                         // bytes between them (4 lanes of 16 bytes)
+  static constexpr int kVTokens = 4 * kHalves, kVWords = kE * kEs / 4;             // tokens and words of a group that a lane reads of the values
+  static constexpr int kScaleRow = D / 32;                                         // scale bytes of a token
+  static constexpr int kQWords = kF32 ? D / 4 : D / 8;
+
+  uint32_t k[kHalves][kKPieces][4];
+  uint32_t v[kVTokens][kNG][kVWords];
+  uint16_t ks[kMx ? kHalves : 1][kMx ? D / 64 : 1];
+  uint32_t vs[kMx ? kHalves : 1][kMx ? kScaleRow : 1];   // 4 tokens' scale bytes
+  uint32_t q[kQWords];
+  f32x4 acc[kNG][kE];
+  float m, l;
+
+  __device__ __forceinline__ void load_q(const char* head_row, int c) {
+    if constexpr (kF32) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(head_row + i * 64 + c * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[4 * i + j] = x[j];
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        // the elements of step s that the keys' lane holds: bf16 32 s + 8 c, 8 bits 64 (s / 2) + 16 c + 8 (s % 2)
+        const int at = kMx ? (s / 2) * 64 + c * 16 + (s % 2) * 8 : s * 32 + c * 8;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(head_row + at * 2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[4 * s + j] = x[j];
+      }
+    }
+  }
+  __device__ __forceinline__ void begin() {
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kNG; ++g)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) acc[g][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // half a's 16 tokens begin at `base` (keys) and `sbase` (their scales); n, c: of the lane
+  __device__ __forceinline__ void load_k(int a, const char* base, const char* sbase, int n, int c) {
+    const uint32_t off = n * kRow + c * 16;
+#pragma unroll
+    for (int i = 0; i < kKPieces; ++i) {
+      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + off + i * kKStep));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[a][i][j] = x[j];
+    }
+    if constexpr (kMx) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) ks[a][i] = *reinterpret_cast<const uint16_t*>(sbase + static_cast<uint32_t>(n * kScaleRow) + 2 * i);
+    }
+  }
+  __device__ __forceinline__ void load_v(int a, const char* base, const char* sbase, int n, int c) {
+    const uint32_t off = c * 4 * kRow + n * kE * kEs;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int g = 0; g < kNG; ++g) load_words(v[4 * a + r][g], base + off + r * kRow + g * kG * kEs);
+    if constexpr (kMx) load_words(vs[a], sbase + static_cast<uint32_t>(c * 4 * kScaleRow));
+  }
+  // eight codes (two words) -> eight bf16
+  static __device__ __forceinline__ bf16x8 decode8(uint32_t w0, uint32_t w1, float s) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
+    return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+  }
+  __device__ __forceinline__ void scores(f32x4 (&s)[kHalves], int c) const {
+#pragma unroll
+    for (int a = 0; a < kHalves; ++a) s[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kKPieces; ++i)
+#pragma unroll
+      for (int a = 0; a < kHalves; ++a) {
+        if constexpr (kF32) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[4 * i + j]), s[a], 0, 0, 0);
+        } else if constexpr (kMx) {
+          const float sc = scale_of((static_cast<uint32_t>(ks[a][i]) >> (8 * (c >> 1))) & 0xFFu);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4 qq = {q[8 * i + 4 * h], q[8 * i + 4 * h + 1], q[8 * i + 4 * h + 2], q[8 * i + 4 * h + 3]};
+            s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, qq), s[a], 0, 0, 0);
+          }
+        } else {
+          const u32x4 kk = {k[a][i][0], k[a][i][1], k[a][i][2], k[a][i][3]}, qq = {q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
+          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, qq), s[a], 0, 0, 0);
+        }
+      }
+  }
+  // p of the scores, with the running maximum, sum and output brought to the new maximum
+  __device__ __forceinline__ void softmax(f32x4 (&s)[kHalves]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int a = 0; a < kHalves; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[a][r]);
+    top = fmaxf(m, row_max4(top));
+    if (__any(top > m)) {
+      const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;   // m = -inf: 0
+      l *= f;
+#pragma unroll
+      for (int g = 0; g < kNG; ++g)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) acc[g][e] *= f;
+      m = top;
+    }
+    const float base = m > -INFINITY ? m : 0.0f;       // all scores so far -inf: p = exp2(-inf) = 0
+#pragma unroll
+    for (int a = 0; a < kHalves; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[a][r] = __builtin_amdgcn_exp2f(s[a][r] - base);
+        l += s[a][r];
+      }
+  }
+  // out += values * p; `mask`: bit 4 a + r set where this lane's token exists (used where CUT)
+  template <bool CUT> __device__ __forceinline__ void output(const f32x4 (&p)[kHalves], uint32_t mask, int n) {
+    if constexpr (kF32) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int g = 0; g < kNG; ++g)
+#pragma unroll
+          for (int e = 0; e < kE; ++e) {
+            const float x = CUT && !((mask >> r) & 1u) ? 0.0f : __uint_as_float(v[r][g][e]);
+            acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[0][r], acc[g][e], 0, 0, 0);
+          }
+    } else {
+      u32x4 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                    // tokens 16 (i / 2) + 4 c + 2 (i % 2) and the next
+        const float x = p[i / 2][2 * (i % 2)], y = p[i / 2][2 * (i % 2) + 1];
+        hi[i] = pack_bf16x2(x, y);
+        lo[i] = pack_bf16x2(x - bf16_lo(hi[i]), y - bf16_hi(hi[i]));
+      }
+      const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
+#pragma unroll
+      for (int g = 0; g < kNG; ++g) {
+        uint32_t w[8][kE / 2];                         // bf16 pairs of the lane's elements, by token
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          if constexpr (kMx) {
+            const int at = (t & 3) * kScaleRow + g * (kG / 32);        // byte of the first of the row's scales for this group
+            const float sc = scale_of((vs[t >> 2][at >> 2] >> (8 * ((at & 3) + n * kE / 32))) & 0xFFu);
+#pragma unroll
+            for (int e = 0; e < kE / 4; ++e) {
+              w[t][2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[t][g][e], sc, false));
+              w[t][2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[t][g][e], sc, true));
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < kE / 2; ++e) w[t][e] = v[t][g][e];
+          }
+          if constexpr (CUT) {
+#pragma unroll
+            for (int e = 0; e < kE / 2; ++e) w[t][e] = (mask >> t) & 1u ? w[t][e] : 0u;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          u32x4 x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)                  // element e of two tokens
+            x[i] = __builtin_amdgcn_perm(w[2 * i + 1][e / 2], w[2 * i][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
+          acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), ph, acc[g][e], 0, 0, 0);
+          acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), pl, acc[g][e], 0, 0, 0);
+        }
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+template <int KIND, int D>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(Args a) {
+  typedef Wave<KIND, D> W;
+  typedef std::conditional_t<KIND == MOE_F32, float, bf16_t> E;
+  constexpr int kPad = D + 4;
+  __shared__ float s_out[kWaves][16][kPad];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ int s_scan[kWaves + 4];
+  const int lane = static_cast<int>(threadIdx.x) & 63, wave = uniform(static_cast<int>(threadIdx.x) >> 6), n = lane & 15, c = lane >> 4;
+  const int units = a.Hkv * a.parts, W_ = static_cast<int>(gridDim.x), me = static_cast<int>(blockIdx.x);
+  const int held = a.max_pages << a.page_shift;
+
+  // tiles of all sequences, and the sequence in which this workgroup's piece begins
+  auto span = [&](int b) { return attn_span(a.lens[b], held, a.window, W::kSub, W::kTile); };
+  int total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    const int b = b0 + static_cast<int>(threadIdx.x);
+    const int nt = b < a.B ? span(b).tiles : 0;
+    const int s = wave_sum_i(nt);
+    __syncthreads();
+    if (lane == 0) s_scan[wave] = s;
+    __syncthreads();
+    total += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
+  }
+  total = uniform(total) * units;
+  const AttnCut cut = attn_cut(total, W_);
+  int at = attn_begin(cut, me);
+  const int end = attn_begin(cut, me + 1);
+  int b_at = 0, before = 0;                            // sequence of tile `at`, tiles (of one unit) of the sequences before it
+  if (at < end) {
+    int run = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+      const int b = b0 + static_cast<int>(threadIdx.x);
+      const int nt = b < a.B ? span(b).tiles : 0;
+      const int incl = wave_inclusive_sum(nt);
+      __syncthreads();
+      if (lane == 63) s_scan[wave] = incl;
+      if (threadIdx.x == 0) s_scan[4] = -1;
+      __syncthreads();
+      int ahead = run + incl - nt;
+      for (int w = 0; w < wave; ++w) ahead += s_scan[w];
+      if (nt > 0 && ahead * units <= at && at < (ahead + nt) * units) { s_scan[4] = b; s_scan[5] = ahead; }
+      __syncthreads();
+      if (s_scan[4] >= 0) { b_at = uniform(s_scan[4]); before = uniform(s_scan[5]); break; }
+      run += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
+    }
+  }
+
+  // sequences without tokens
+  for (int b = me; b < a.B; b += W_) {
+    if (span(b).tiles != 0) continue;
+    for (int i = threadIdx.x; i < a.Hq * D; i += kThreads) static_cast<E*>(a.out)[static_cast<int64_t>(b) * a.Hq * D + i] = 0;
+    if (a.lse)
+      for (int i = threadIdx.x; i < a.Hq; i += kThreads) a.lse[static_cast<int64_t>(b) * a.Hq + i] = -INFINITY;
+    if (a.unit_pieces)
+      for (int i = threadIdx.x; i < units; i += kThreads) a.unit_pieces[2 * (static_cast<int64_t>(b) * units + i)] = -1;
+  }
+
+  W w;
+  while (at < end) {
+    AttnSpan sp = span(b_at);
+    while (at >= (before + sp.tiles) * units) {        // on to the sequence that has the tile
+      before += sp.tiles;
+      sp = span(++b_at);
+    }
+    const int u = (at - before * units) / sp.tiles, unit_begin = before * units + u * sp.tiles, unit_end = unit_begin + sp.tiles;
+    const int first = at, last = min(end, unit_end);
+    const int kv = u / a.parts, part = u - kv * a.parts, head0 = kv * a.group + part * a.heads, heads = min(a.heads, a.group - part * a.heads);
+    const int lo = sp.lo, len = sp.len;
+
+    {
+      const int h = head0 + min(n, heads - 1);         // columns without a head repeat the last one's
+      w.load_q(static_cast<const char*>(a.q) + (static_cast<int64_t>(b_at) * a.q_stride_b + static_cast<int64_t>(h) * a.q_stride_h) * static_cast<int>(sizeof(E)), c);
+    }
+    w.begin();
+    const int32_t* pages = a.block_table + static_cast<int64_t>(b_at) * a.max_pages;
+    const int page_mask = (1 << a.page_shift) - 1;
+    // bases of a half of 16 tokens that begins at token t; a half without tokens takes the nearest one that has some, and is masked
+    auto place = [&](int t, int64_t& rows, int64_t& scales) {
+      const int near = min(max(t, lo), len - 1);
+      const int page = min(max(uniform(pages[near >> a.page_shift]), 0), a.pages - 1);
+      const int row = (kv << a.page_shift) + (near & page_mask & ~15);
+      rows = page * a.page_bytes + static_cast<int64_t>(row) * W::kRow;
+      scales = page * a.scale_page_bytes + static_cast<int64_t>(row) * W::kScaleRow;
+    };
+    auto token = [&](int tile) { return sp.base + (tile - unit_begin) * W::kTile + wave * W::kSub; };
+    int64_t row_at[W::kHalves], scale_at[W::kHalves], next_row[W::kHalves], next_scale[W::kHalves];
+    int t0 = token(first);
+    const bool any = t0 < len;
+    if (any) {
+#pragma unroll
+      for (int h = 0; h < W::kHalves; ++h) {
+        place(t0 + 16 * h, row_at[h], scale_at[h]);
+        w.load_k(h, a.k + row_at[h], a.ks + scale_at[h], n, c);
+        w.load_v(h, a.v + row_at[h], a.vs + scale_at[h], n, c);
+      }
+      for (int tile = first;;) {
+        const int t1 = token(tile + 1);
+        const bool more = tile + 1 < last && t1 < len;
+        if (more) {
+#pragma unroll
+          for (int h = 0; h < W::kHalves; ++h) place(t1 + 16 * h, next_row[h], next_scale[h]);
+        }
+        f32x4 s[W::kHalves];
+        w.scores(s, c);
+        if (more) {
+#pragma unroll
+          for (int h = 0; h < W::kHalves; ++h) w.load_k(h, a.k + next_row[h], a.ks + next_scale[h], n, c);
+        }
+        const bool whole = t0 >= lo && t0 + W::kSub <= len;
+        uint32_t mask = 0xFFu;
+        if (whole) {
+#pragma unroll
+          for (int h = 0; h < W::kHalves; ++h) s[h] *= a.scale_log2;
+        } else {
+          mask = 0u;
+#pragma unroll
+          for (int h = 0; h < W::kHalves; ++h)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int t = t0 + 16 * h + 4 * c + r;
+              const bool there = t >= lo && t < len;
+              mask |= there ? 1u << (4 * h + r) : 0u;
+              s[h][r] = there ? s[h][r] * a.scale_log2 : -INFINITY;
+            }
+        }
+        w.softmax(s);
+        if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
+        if (!more) break;
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + next_row[h], a.vs + next_scale[h], n, c);
+        ++tile;
+        t0 = t1;
+      }
+    }
+
+    // the four waves' parts, and out
+    const float l = row_sum4(w.l);
+    __syncthreads();                                   // the last piece's sums have been read
+    if (lane < 16) { s_m[wave][n] = w.m; s_l[wave][n] = l; }
+    __syncthreads();
+    {
+      const float m = fmaxf(fmaxf(s_m[0][n], s_m[1][n]), fmaxf(s_m[2][n], s_m[3][n]));
+      const float f = w.m > -INFINITY ? __builtin_amdgcn_exp2f(w.m - m) : 0.0f;
+      if (n < heads) {
+#pragma unroll
+        for (int g = 0; g < W::kNG; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < W::kE; e += 4) {
+              const f32x4 x = {w.acc[g][e][r] * f, w.acc[g][e + 1][r] * f, w.acc[g][e + 2][r] * f, w.acc[g][e + 3][r] * f};
+              *reinterpret_cast<f32x4*>(&s_out[wave][n][g * W::kG + (4 * c + r) * W::kE + e]) = x;
+            }
+      }
+    }
+    __syncthreads();
+    const bool complete = first == unit_begin && last == unit_end;
+    const int slot = 2 * me + (first == attn_begin(cut, me) ? 0 : 1);
+    for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
+      const int h = i / (D / 4), d = (i - h * (D / 4)) * 4;
+      const float m = fmaxf(fmaxf(s_m[0][h], s_m[1][h]), fmaxf(s_m[2][h], s_m[3][h]));
+      float sum = 0.0f;
+      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        sum += s_m[v][h] > -INFINITY ? s_l[v][h] * __builtin_amdgcn_exp2f(s_m[v][h] - m) : s_l[v][h];
+        o += *reinterpret_cast<const f32x4*>(&s_out[v][h][d]);
+      }
+      if (complete) {
+        const int64_t row = static_cast<int64_t>(b_at) * a.Hq + head0 + h;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if constexpr (KIND == MOE_F32) {
+          *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + row * D + d) = o * inv;
+        } else {
+          *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(a.out) + row * D + d) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+        }
+        if (a.lse && d == 0) a.lse[row] = (m + log2f(sum)) * kLn2;
+      } else {
+        float* to = a.slots + (static_cast<int64_t>(slot) * a.heads + h) * (D + 4);
+        *reinterpret_cast<f32x4*>(to + 4 + d) = o;
+        if (d == 0) { to[0] = m; to[1] = sum; }
+      }
+    }
+    if (a.unit_pieces && threadIdx.x == 0 && first == unit_begin) {
+      int32_t* p = a.unit_pieces + 2 * (static_cast<int64_t>(b_at) * units + u);
+      p[0] = complete ? -1 : slot;
+      p[1] = attn_owner(cut, unit_end - 1);
+    }
+    at = last;
+  }
+}
+
+// ---- pieces of a context joined: a workgroup per sequence and head ---------------------------------------
+template <int KIND, int D>
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a) {
+  typedef std::conditional_t<KIND == MOE_F32, float, bf16_t> E;
+  constexpr int kCols = D / 4, kSlices = kThreads / kCols;
+  __shared__ float s_f[kAttnMaxBlocks + 1];
+  __shared__ float s_red[2 * kWaves];
+  __shared__ float s_out[kSlices][D];
+  const int units = a.Hkv * a.parts, tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int b = blockIdx.x / a.Hq, head = blockIdx.x - b * a.Hq, kv = head / a.group, in_group = head - kv * a.group;
+  const int part = in_group / a.heads, h = in_group - part * a.heads;
+  const int32_t* p = a.unit_pieces + 2 * (static_cast<int64_t>(b) * units + kv * a.parts + part);
+  const int slot0 = p[0];
+  if (slot0 < 0) return;
+  const int w0 = slot0 >> 1, count = min(p[1] - w0 + 1, kAttnMaxBlocks);
+  // the first piece may be its workgroup's second; all others are their workgroup's first
+  auto piece = [&](int i) { return a.slots + (static_cast<int64_t>(i == 0 ? slot0 : 2 * (w0 + i)) * a.heads + h) * (D + 4); };
+  float top = -INFINITY;
+  for (int i = tid; i < count; i += kThreads) {
+    s_f[i] = piece(i)[0];
+    top = fmaxf(top, s_f[i]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if (lane == 0) s_red[wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+  float sum = 0.0f;
+  for (int i = tid; i < count; i += kThreads) {
+    const float m = s_f[i], f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
+    sum += piece(i)[1] * f;
+    s_f[i] = f;
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) s_red[kWaves + wave] = sum;
+  __syncthreads();
+  sum = (s_red[kWaves] + s_red[kWaves + 1]) + (s_red[kWaves + 2] + s_red[kWaves + 3]);
+  const int slice = tid / kCols, d = (tid - slice * kCols) * 4;
+  if (slice < kSlices) {
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int i = slice; i < count; i += kSlices) o += *reinterpret_cast<const f32x4*>(piece(i) + 4 + d) * s_f[i];
+    *reinterpret_cast<f32x4*>(&s_out[slice][d]) = o;
+  }
+  __syncthreads();
+  if (tid < kCols) {
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s) o += *reinterpret_cast<const f32x4*>(&s_out[s][d]);
+    const int64_t row = static_cast<int64_t>(b) * a.Hq + head;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if constexpr (KIND == MOE_F32) {
+      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + row * D + d) = o * inv;
+    } else {
+      *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(a.out) + row * D + d) = u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+    }
+    if (a.lse && d == 0) a.lse[row] = (top + log2f(sum)) * kLn2;
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------
+// Tiles of a context of the whole page table, and the grid: never more workgroups than tiles, nor than kAttnMaxBlocks.
+struct Launch { int tile, parts, heads, blocks; int64_t most_tiles; bool cut; };
+Launch launch_of(int dtype, int B, int Hq, int Hkv, int page_size, int max_pages) {
+  Launch l;
+  l.tile = kWaves * (dtype == MOE_F32 ? 16 : 32);
+  const int group = Hq / Hkv;
+  l.parts = ceil_div(group, 16);
+  l.heads = ceil_div(group, l.parts);
+  const int64_t held = static_cast<int64_t>(page_size) * max_pages, tiles = (held + l.tile - 1) / l.tile + 1;   // a window may begin inside a tile
+  l.most_tiles = tiles * B * Hkv * l.parts;
+  l.blocks = static_cast<int>(l.most_tiles < kAttnMaxBlocks ? l.most_tiles : kAttnMaxBlocks);
+  if (l.blocks < 1) l.blocks = 1;
+  l.cut = held > l.tile;
+  return l;
+}
+// the larger of the element types' workspaces: the query does not know the cache's type
+size_t pieces_bytes(int B, int Hkv, int parts) { return align_up(static_cast<size_t>(B) * Hkv * parts * 2 * sizeof(int32_t), 16); }
+size_t ws_bytes_of(const Launch& l, int B, int Hkv, int dim) {
+  return pieces_bytes(B, Hkv, l.parts) + static_cast<size_t>(l.blocks) * 2 * l.heads * (dim + 4) * sizeof(float);
+}
+
+template <int KIND, int D> void launch_decode(const Args& a, const Launch& l, hipStream_t st) {
+  MOE_LAUNCH("attn_decode", (attn_decode_kernel<KIND, D>), dim3(l.blocks), dim3(kThreads), 0, st, a);
+  if (l.cut) MOE_LAUNCH("attn_join", (attn_join_kernel<KIND, D>), dim3(static_cast<unsigned>(a.B) * a.Hq), dim3(kThreads), 0, st, a);
+}
+template <int KIND> void launch_decode_dim(int dim, const Args& a, const Launch& l, hipStream_t st) {
+  if (dim == 64) launch_decode<KIND, 64>(a, l, st);
+  else if (dim == 128) launch_decode<KIND, 128>(a, l, st);
+  else if (dim == 192) launch_decode<KIND, 192>(a, l, st);
+  else launch_decode<KIND, 256>(a, l, st);
+}
+
+}  // namespace
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" size_t moe_paged_attn_decode_workspace_bytes(int B, int Hq, int heads, int dim, int page_size, int max_pages) {
+  if (B <= 0 || Hq <= 0 || heads <= 0 || dim <= 0 || page_size <= 0 || max_pages <= 0 || Hq % heads != 0) return 256;
+  const size_t f32 = ws_bytes_of(launch_of(MOE_F32, B, Hq, heads, page_size, max_pages), B, heads, dim);
+  const size_t bf16 = ws_bytes_of(launch_of(MOE_BF16, B, Hq, heads, page_size, max_pages), B, heads, dim);
+  return f32 > bf16 ? f32 : bf16;
+}
+
+extern "C" int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int64_t q_stride_h, const moe_kv_cache_t* cache,
+                                         const int32_t* block_table, int max_pages, const int32_t* lens, int B, int Hq, float scale,
+                                         int window, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  if (int32_t rc = check_cache("paged_attn_decode", cache)) return rc;
+  MOE_REQUIRE(B >= 0 && Hq > 0 && max_pages >= 0 && window >= 0, MOE_ERR_INVALID_ARG, "paged_attn_decode: need B, max_pages, window >= 0 and Hq > 0 (B=%d Hq=%d max_pages=%d window=%d)",
+              B, Hq, max_pages, window);
+  MOE_REQUIRE(Hq % cache->heads == 0, MOE_ERR_INVALID_ARG, "paged_attn_decode: Hq=%d is no multiple of the cache's %d heads", Hq, cache->heads);
+  MOE_REQUIRE(std::isfinite(scale), MOE_ERR_INVALID_ARG, "paged_attn_decode: scale is not finite");
+  if (B == 0) return MOE_OK;
+  const int el = cache->dtype == MOE_F32 ? 4 : 2;
+  MOE_REQUIRE(q && lens && out && (max_pages == 0 || block_table), MOE_ERR_INVALID_ARG, "paged_attn_decode: null pointer");
+  MOE_REQUIRE(aligned16(q) && aligned16(out) && aligned16(lse), MOE_ERR_INVALID_ARG, "paged_attn_decode: tensors must be 16-byte aligned");
+  MOE_REQUIRE(q_stride_b % (16 / el) == 0 && q_stride_h % (16 / el) == 0, MOE_ERR_INVALID_ARG, "paged_attn_decode: strides must be multiples of 16 bytes");
+  MOE_REQUIRE(static_cast<int64_t>(cache->page_size) * max_pages < (int64_t{1} << 31) - 4096, MOE_ERR_UNSUPPORTED, "paged_attn_decode: contexts of %lld tokens",
+              static_cast<long long>(cache->page_size) * max_pages);
+  MOE_REQUIRE(static_cast<int64_t>(B) * Hq <= (1 << 23), MOE_ERR_UNSUPPORTED, "paged_attn_decode: B * Hq = %lld above 2^23", static_cast<long long>(B) * Hq);
+  const Launch l = launch_of(cache->dtype, B, Hq, cache->heads, cache->page_size, max_pages);
+  MOE_REQUIRE(l.most_tiles < (int64_t{1} << 31) - 65536, MOE_ERR_UNSUPPORTED, "paged_attn_decode: %lld tiles of %d tokens", static_cast<long long>(l.most_tiles), l.tile);
+  const size_t need = moe_paged_attn_decode_workspace_bytes(B, Hq, cache->heads, cache->dim, cache->page_size, max_pages);
+  MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "paged_attn_decode: workspace null, misaligned or smaller than %zu bytes", need);
+  Args a{};
+  a.q = q; a.q_stride_b = q_stride_b; a.q_stride_h = q_stride_h;
+  a.k = static_cast<const char*>(cache->k); a.v = static_cast<const char*>(cache->v);
+  a.ks = static_cast<const char*>(cache->k_scales); a.vs = static_cast<const char*>(cache->v_scales);
+  a.page_bytes = cache->page_stride * (cache->dtype == MOE_F32 ? 4 : cache->dtype == MOE_BF16 ? 2 : 1);
+  a.scale_page_bytes = cache->scale_page_stride;
+  a.pages = cache->pages; a.page_shift = __builtin_ctz(cache->page_size);
+  a.block_table = block_table; a.lens = lens; a.max_pages = max_pages; a.B = B; a.Hq = Hq; a.Hkv = cache->heads; a.group = Hq / cache->heads;
+  a.parts = l.parts; a.heads = l.heads; a.scale_log2 = scale * kLog2e; a.window = window; a.out = out; a.lse = lse;
+  if (l.cut) {
+    a.unit_pieces = static_cast<int32_t*>(ws);
+    a.slots = reinterpret_cast<float*>(static_cast<char*>(ws) + pieces_bytes(B, cache->heads, l.parts));
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  begin_call("moe_paged_attn_decode", st);
+  if (cache->dtype == MOE_F32) launch_decode_dim<MOE_F32>(cache->dim, a, l, st);
+  else if (cache->dtype == MOE_BF16) launch_decode_dim<MOE_BF16>(cache->dim, a, l, st);
+  else launch_decode_dim<MOE_MX8>(cache->dim, a, l, st);
+  return end_call();
+}

@@ -1,0 +1,28 @@
+// Which workgroup sees which tokens in the attention of one token over a paged cache: integer arithmetic without anything of a GPU in it,
+// so that a plain C++ program can enumerate it (tests/test_attn_plan.py).
+#pragma once
+#include <stdint.h>
+
+namespace moe {
+
+constexpr int kAttnMaxBlocks = 512;                    // workgroups of a launch
+
+// Tokens [lo, len) of a sequence are seen, in `tiles` tiles of `tile` tokens from `base` on, a multiple of `sub` at or below lo.
+struct AttnSpan { int lo, len, base, tiles; };
+constexpr AttnSpan attn_span(int len, int held, int window, int sub, int tile) {
+  const int n = len < 0 ? 0 : len < held ? len : held;
+  const int lo = window > 0 && n > window ? n - window : 0, base = lo / sub * sub;
+  return AttnSpan{lo, n, base, (n - base + tile - 1) / tile};
+}
+
+// `total` tiles on `blocks` workgroups: the first `longer` of them take size + 1, the others size.
+struct AttnCut { int size, longer; };
+constexpr AttnCut attn_cut(int total, int blocks) { return AttnCut{total / blocks, total % blocks}; }
+constexpr int attn_begin(const AttnCut& c, int block) { return block * c.size + (block < c.longer ? block : c.longer); }
+// the workgroup that has a tile
+constexpr int attn_owner(const AttnCut& c, int tile) {
+  const int in_longer = c.longer * (c.size + 1);
+  return tile < in_longer ? tile / (c.size + 1) : c.longer + (tile - in_longer) / (c.size > 0 ? c.size : 1);
+}
+
+}  // namespace moe

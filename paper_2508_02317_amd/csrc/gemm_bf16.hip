@@ -37,6 +37,7 @@
 #include <utility>
 #include "launch_plan.h"
 #include "moe_common.h"
+#include "mx8_codes.h"
 
 namespace moe {
 

@@ -239,4 +239,27 @@ void router_bwd_bf16(const RouterBwdArgs& a);
 void router_fwd_f32(const RouterFwdArgs& a);
 void router_bwd_f32(const RouterBwdArgs& a);
 
+// ---- rotary positions, paged key/value cache (rope.hip), attention of one token over it (attn_decode.hip) ----
+int32_t check_cache(const char* who, const moe_kv_cache_t* c);   // MOE_OK, or why the descriptor cannot be used
+struct RotateArgs {
+  const void *q, *k, *v;              // [T, Hq, D], [T, Hk, D], [T, Hv, D], strides in elements, the last one 1
+  int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h, v_stride_t, v_stride_h;
+  int T, Hq, Hk, Hv, D, rot;
+  const int32_t* positions;           // [T]
+  const float *cos, *sin;             // [n_pos, rot / 2]
+  int n_pos, interleaved, back;
+  void *q_out, *k_out;                // k_out: not with a cache
+  int64_t qo_stride_t, qo_stride_h, ko_stride_t, ko_stride_h;
+  const int64_t* slots;               // [T], with a cache
+  moe_kv_cache_t cache;
+  hipStream_t stream;
+};
+struct CacheReadArgs {
+  moe_kv_cache_t cache;
+  const int32_t *block_table, *row_start, *first;   // [B, max_pages], [B + 1], [B] or null
+  void *k_out, *v_out;
+  int max_pages, B, rows;
+  hipStream_t stream;
+};
+
 }  // namespace moe

@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoe_gfx950.so")
 
 MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP = range(5)
-MOE_F32, MOE_BF16 = 0, 1
+MOE_F32, MOE_BF16, MOE_MX8 = 0, 1, 2
 
 EXPORTS = [
     "moe_version", "moe_last_error",
@@ -32,12 +32,21 @@ EXPORTS = [
     "moe_router_logits_workspace_bytes", "moe_router_logits", "moe_router_bwd_workspace_bytes", "moe_router_bwd",
     "moe_mx8_quantise", "moe_grouped_gemm_swiglu_fwd_mx8_workspace_bytes", "moe_grouped_gemm_swiglu_fwd_mx8",
     "moe_grouped_gemm_down_mx8",
+    "moe_rope_table", "moe_rope_fwd", "moe_rope_bwd", "moe_kv_cache_write", "moe_kv_cache_read",
+    "moe_paged_attn_decode_workspace_bytes", "moe_paged_attn_decode",
     "moe_set_launch_hook",
 ]
 
 
 # void hook(const char* kernel_name, int phase, void* stream, void* user)
 LAUNCH_HOOK = ctypes.CFUNCTYPE(None, ctypes.c_char_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p)
+
+
+class moe_kv_cache_t(ctypes.Structure):
+    """The cache descriptor of include/moe.h."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "pages", "heads", "page_size", "dim", "reserved")] +
+                [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales")] +
+                [(n, ctypes.c_int64) for n in ("page_stride", "scale_page_stride")])
 
 
 class MoEError(RuntimeError):
@@ -111,6 +120,20 @@ def _load():
     lib.moe_grouped_gemm_swiglu_fwd_mx8.argtypes = [vp, vp, i32, i32, vp] + [vp] * 6 + [i32] * 4 + [vp] * 5 + [sz, vp]
     lib.moe_grouped_gemm_down_mx8.restype = ctypes.c_int32
     lib.moe_grouped_gemm_down_mx8.argtypes = [vp] * 4 + [i32] * 4 + [vp] * 3 + [sz, vp]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.moe_rope_table.restype = ctypes.c_int32
+    lib.moe_rope_table.argtypes = [vp, i32, i32, ctypes.c_double, vp, vp, vp]
+    for turn in (lib.moe_rope_fwd, lib.moe_rope_bwd):
+        turn.restype = ctypes.c_int32
+        turn.argtypes = [vp, i64, i64] * 2 + [i32] * 6 + [vp] * 3 + [i32] * 2 + [vp, i64, i64] * 2 + [vp]
+    lib.moe_kv_cache_write.restype = ctypes.c_int32
+    lib.moe_kv_cache_write.argtypes = [vp] + [vp, i64, i64] * 2 + [i32, vp] + [vp, i64, i64] + [i32] * 2 + [vp] * 3 + [i32] * 2 + [vp, i64, i64, vp]
+    lib.moe_kv_cache_read.restype = ctypes.c_int32
+    lib.moe_kv_cache_read.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp]
+    lib.moe_paged_attn_decode_workspace_bytes.restype = sz
+    lib.moe_paged_attn_decode_workspace_bytes.argtypes = [i32] * 6
+    lib.moe_paged_attn_decode.restype = ctypes.c_int32
+    lib.moe_paged_attn_decode.argtypes = [vp, i64, i64, vp, vp, i32, vp, i32, i32, f32, i32, vp, vp, vp, sz, vp]
     lib.moe_set_launch_hook.restype = ctypes.c_int32
     lib.moe_set_launch_hook.argtypes = [LAUNCH_HOOK, vp]
     return lib
@@ -454,3 +477,176 @@ def moe_router_bwd(dlogits, x, w_router, dx=None, out_dw=None, ws=None):
                               _ptr(ws), n, _stream()))
     return dx, out_dw
 
+
+# ---- rotary positions, the paged key/value cache, attention of one token over it -----------------------------------
+
+def _heads(t, dtype, name, shape=None):
+    """A [T, heads, dim] device tensor whose heads are contiguous: its pointer and the strides of tokens and heads."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError("%s must be a [tokens, heads, dim] device tensor" % name)
+    st, sh, se = t.stride()
+    if se != 1 and t.shape[2] != 1:
+        raise ValueError("%s: the elements of a head must be contiguous" % name)
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t.data_ptr(), st, sh
+
+
+def _table(cos, sin, positions, T):
+    """rot, n_pos and the pointers of a rotation's table and positions; cos None: no rotation."""
+    if cos is None:
+        return 0, 0, None, None, None
+    _need(cos, torch.float32, "cos"); _need(sin, torch.float32, "sin"); _need(positions, torch.int32, "positions")
+    if cos.dim() != 2 or cos.shape != sin.shape or positions.numel() != T:
+        raise ValueError("cos and sin must be [n_pos, rot / 2] and positions [%d], got %s, %s and %s"
+                         % (T, tuple(cos.shape), tuple(sin.shape), tuple(positions.shape)))
+    return 2 * cos.shape[1], cos.shape[0], positions.data_ptr(), cos.data_ptr(), sin.data_ptr()
+
+
+def moe_rope_table(freq, n_pos, amplitude=1.0, out=None):
+    """freq [half] f64 -> cos, sin [n_pos, half] f32 of the angles p * freq[i], times amplitude."""
+    _need(freq, torch.float64, "freq")
+    if out is None:
+        out = tuple(torch.empty((n_pos, freq.numel()), dtype=torch.float32, device=freq.device) for _ in range(2))
+    cos, sin = out
+    _need(cos, torch.float32, "cos"); _need(sin, torch.float32, "sin")
+    if cos.shape != (n_pos, freq.numel()) or sin.shape != cos.shape:
+        raise ValueError("out must be two tensors [%d, %d]" % (n_pos, freq.numel()))
+    _check(lib.moe_rope_table(_ptr(freq), n_pos, freq.numel(), amplitude, _ptr(cos), _ptr(sin), _stream()))
+    return cos, sin
+
+
+def _rope(call, q, k, positions, cos, sin, interleaved, out):
+    some = q if q is not None else k
+    T, _, D = some.shape
+    code, dtype = _dtype_code(some), some.dtype
+    if out is None:
+        out = tuple(None if t is None else torch.empty(t.shape, dtype=dtype, device=some.device) for t in (q, k))
+    args, heads = [], []
+    for t, o, name in ((q, out[0], "q"), (k, out[1], "k")):
+        if t is None:
+            args.append(((None, 0, 0), (None, 0, 0)))
+            heads.append(0)
+            continue
+        shape = t.shape
+        if shape[0] != T or shape[2] != D:
+            raise ValueError("q and k must have the same tokens and head size")
+        args.append((_heads(t, dtype, name), _heads(o, dtype, name + " out", shape)))
+        heads.append(shape[1])
+    rot, n_pos, p_pos, p_cos, p_sin = _table(cos, sin, positions, T)
+    (qi, qo), (ki, ko) = args
+    _check(call(*qi, *ki, code, T, heads[0], heads[1], D, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, *ko, _stream()))
+    return out
+
+
+def moe_rope_fwd(q, k, positions, cos, sin, interleaved=False, out=None):
+    """q [T, Hq, D], k [T, Hk, D] (either may be None) rotated by positions [T] i32 with the table cos, sin [n_pos, rot / 2] f32.
+    -> q_out, k_out; out = (q, k) rotates in place."""
+    return _rope(lib.moe_rope_fwd, q, k, positions, cos, sin, interleaved, out)
+
+
+def moe_rope_bwd(dq, dk, positions, cos, sin, interleaved=False, out=None):
+    """Gradients of moe_rope_fwd's inputs from those of its outputs."""
+    return _rope(lib.moe_rope_bwd, dq, dk, positions, cos, sin, interleaved, out)
+
+
+class KVCacheView:
+    """A paged cache as the calls below take it: the tensors it lies in and their descriptor, made once."""
+
+    def __init__(self, k, v, k_scales=None, v_scales=None):
+        if k.dtype is torch.uint8:
+            code, self.dtype = MOE_MX8, torch.bfloat16
+        else:
+            code, self.dtype = _dtype_code(k), k.dtype
+        pages, heads, page_size, dim = k.shape
+        for name, t, row in (("k", k, dim), ("v", v, dim)) + ((("k_scales", k_scales, dim // 32), ("v_scales", v_scales, dim // 32)) if code == MOE_MX8 else ()):
+            if t is None or not t.is_cuda or t.dtype is not (torch.uint8 if name.endswith("scales") else k.dtype):
+                raise ValueError("%s must be a device tensor, uint8 for scales and the type of k otherwise" % name)
+            if t.shape != (pages, heads, page_size, row) or t.stride()[1:] != (page_size * row, row, 1):
+                raise ValueError("%s must be [pages, heads, page_size, %d] = %s, dense within a page" % (name, row, (pages, heads, page_size, row)))
+        if v.stride(0) != k.stride(0) or (code == MOE_MX8 and v_scales.stride(0) != k_scales.stride(0)):
+            raise ValueError("keys and values must have the same stride between pages")
+        if code != MOE_MX8 and (k_scales is not None or v_scales is not None):
+            raise ValueError("scales belong to a cache of 8-bit codes")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.heads, self.dim, self.page_size = heads, dim, page_size
+        self.desc = moe_kv_cache_t(code, pages, heads, page_size, dim, 0, _ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), k.stride(0),
+                                   k_scales.stride(0) if code == MOE_MX8 else 0)
+        self.ref = ctypes.addressof(self.desc)
+
+
+def moe_kv_cache(k, v, k_scales=None, v_scales=None):
+    """k, v [pages, heads, page_size, dim] f32, bf16, or uint8 codes with scales uint8 [pages, heads, page_size, dim / 32].
+    -> the view of them that moe_kv_cache_write, moe_kv_cache_read and moe_paged_attn_decode take (it keeps the tensors)."""
+    return KVCacheView(k, v, k_scales, v_scales)
+
+
+def moe_kv_cache_write(cache, k, v, slots, q=None, positions=None, cos=None, sin=None, interleaved=False, q_out=None):
+    """k, v [T, heads, dim] into the cache at slots [T] i64, the keys rotated if a table is given; q [T, Hq, dim] rotated into q_out.
+    -> q_out (None without q)."""
+    T, dt = k.shape[0], cache.dtype
+    shape = (T, cache.heads, cache.dim)
+    ki, vi = _heads(k, dt, "k", shape), _heads(v, dt, "v", shape)
+    _need(slots, torch.int64, "slots")
+    if slots.numel() != T:
+        raise ValueError("slots must be [%d]" % T)
+    qi, qo, Hq = (None, 0, 0), (None, 0, 0), 0
+    if q is not None:
+        Hq = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=q.device)
+        qi, qo = _heads(q, dt, "q", (T, Hq, cache.dim)), _heads(q_out, dt, "q_out", q.shape)
+    rot, n_pos, p_pos, p_cos, p_sin = _table(cos, sin, positions, T)
+    _check(lib.moe_kv_cache_write(cache.ref, *ki, *vi, T, slots.data_ptr(), *qi, Hq, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, _stream()))
+    return q_out
+
+
+def moe_kv_cache_read(cache, pages, row_start, rows=None, first=None, out=None):
+    """Tokens first[b] .. of every sequence b (first None: from its first on) into the rows row_start[b] .. row_start[b + 1] - 1.
+    pages [B, max_pages] i32, row_start [B + 1] i32, first [B] i32; rows: row_start[B], needed without out.
+    -> k, v [rows, heads, dim] in the cache's type (bf16 for 8-bit codes)."""
+    _need(pages, torch.int32, "pages"); _need(row_start, torch.int32, "row_start")
+    B, max_pages = pages.shape
+    if row_start.numel() != B + 1:
+        raise ValueError("row_start must be [%d]" % (B + 1))
+    if first is not None:
+        _need(first, torch.int32, "first")
+        if first.numel() != B:
+            raise ValueError("first must be [%d]" % B)
+    if out is None:
+        if rows is None:
+            raise ValueError("rows (the last of row_start, on the host) or out must be given")
+        out = tuple(torch.empty((rows, cache.heads, cache.dim), dtype=cache.dtype, device=pages.device) for _ in range(2))
+    k, v = out
+    _need(k, cache.dtype, "k out"); _need(v, cache.dtype, "v out")
+    if k.dim() != 3 or k.shape[1:] != (cache.heads, cache.dim) or v.shape != k.shape:
+        raise ValueError("out must be two tensors [rows, %d, %d]" % (cache.heads, cache.dim))
+    _check(lib.moe_kv_cache_read(cache.ref, pages.data_ptr(), max_pages, row_start.data_ptr(), _ptr(first), B, k.shape[0], k.data_ptr(), v.data_ptr(),
+                                 _stream()))
+    return out
+
+
+def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None, lse=None, ws=None):
+    """Attention of one token per sequence: q [B, Hq, dim] over the first lens[b] tokens of the pages pages[b, :] (the last `window` of them
+    where it is not 0).  scale None: dim ** -0.5.  -> out [B, Hq, dim], lse [B, Hq] f32 (None where lse is not given; True makes one)."""
+    dt = cache.dtype
+    B, Hq, _ = q.shape
+    qi = _heads(q, dt, "q", (B, Hq, cache.dim))
+    _need(pages, torch.int32, "pages"); _need(lens, torch.int32, "lens")
+    if pages.dim() != 2 or pages.shape[0] != B or lens.numel() != B:
+        raise ValueError("pages must be [%d, max_pages] and lens [%d]" % (B, B))
+    if out is None:
+        out = torch.empty((B, Hq, cache.dim), dtype=dt, device=q.device)
+    elif _need(out, dt, "out").shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    if lse is True:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    elif lse is not None and _need(lse, torch.float32, "lse").shape != (B, Hq):
+        raise ValueError("lse must be [%d, %d]" % (B, Hq))
+    max_pages = pages.shape[1]
+    ws, nbytes = _ws(lib.moe_paged_attn_decode_workspace_bytes, (B, Hq, cache.heads, cache.dim, cache.page_size, max_pages), ws, q.device)
+    _check(lib.moe_paged_attn_decode(*qi, cache.ref, pages.data_ptr(), max_pages, lens.data_ptr(), B, Hq,
+                                     cache.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse), ws.data_ptr(), nbytes, _stream()))
+    return out, lse
