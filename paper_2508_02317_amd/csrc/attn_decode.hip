@@ -81,19 +81,19 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
   if constexpr (N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
-      const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
     }
   } else if constexpr (N % 2 == 0) {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-      const u32x2 x = reinterpret_cast<const u32x2*>(p)[i];
+      const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p) + i);
       w[2 * i] = x[0]; w[2 * i + 1] = x[1];
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    for (int i = 0; i < N; ++i) w[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p) + i);
   }
 }
 
@@ -278,10 +278,14 @@ template <int KIND, int D> struct Wave {
   }
 };
 
+// Integers that no launch of the call writes, read by scalar loads (a vector load among those of the cache would have to be waited for with them).
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar_ints(const int32_t* p) { return reinterpret_cast<ScalarInts>(reinterpret_cast<uintptr_t>(p)); }
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int KIND, int D>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(Args a) {
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_kernel(Args a) {
   typedef Wave<KIND, D> W;
   typedef std::conditional_t<KIND == MOE_F32, float, bf16_t> E;
   constexpr int kPad = D + 4;
@@ -294,6 +298,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
 
   // tiles of all sequences, and the sequence in which this workgroup's piece begins
   auto span = [&](int b) { return attn_span(a.lens[b], held, a.window, W::kSub, W::kTile); };
+  const ScalarInts lens = scalar_ints(a.lens);
+  auto span_of = [&](int b) { return attn_span(lens[b], held, a.window, W::kSub, W::kTile); };   // b the same in all lanes
   int total = 0;
   for (int b0 = 0; b0 < a.B; b0 += kThreads) {
     const int b = b0 + static_cast<int>(threadIdx.x);
@@ -330,7 +336,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
 
   // sequences without tokens
   for (int b = me; b < a.B; b += W_) {
-    if (span(b).tiles != 0) continue;
+    if (span_of(b).tiles != 0) continue;
     for (int i = threadIdx.x; i < a.Hq * D; i += kThreads) static_cast<E*>(a.out)[static_cast<int64_t>(b) * a.Hq * D + i] = 0;
     if (a.lse)
       for (int i = threadIdx.x; i < a.Hq; i += kThreads) a.lse[static_cast<int64_t>(b) * a.Hq + i] = -INFINITY;
@@ -340,10 +346,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
 
   W w;
   while (at < end) {
-    AttnSpan sp = span(b_at);
+    AttnSpan sp = span_of(b_at);
     while (at >= (before + sp.tiles) * units) {        // on to the sequence that has the tile
       before += sp.tiles;
-      sp = span(++b_at);
+      sp = span_of(++b_at);
     }
     const int u = (at - before * units) / sp.tiles, unit_begin = before * units + u * sp.tiles, unit_end = unit_begin + sp.tiles;
     const int first = at, last = min(end, unit_end);
@@ -355,39 +361,46 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       w.load_q(static_cast<const char*>(a.q) + (static_cast<int64_t>(b_at) * a.q_stride_b + static_cast<int64_t>(h) * a.q_stride_h) * static_cast<int>(sizeof(E)), c);
     }
     w.begin();
-    const int32_t* pages = a.block_table + static_cast<int64_t>(b_at) * a.max_pages;
+    const ScalarInts pages = scalar_ints(a.block_table + static_cast<int64_t>(b_at) * a.max_pages);
     const int page_mask = (1 << a.page_shift) - 1;
-    // bases of a half of 16 tokens that begins at token t; a half without tokens takes the nearest one that has some, and is masked
-    auto place = [&](int t, int64_t& rows, int64_t& scales) {
-      const int near = min(max(t, lo), len - 1);
-      const int page = min(max(uniform(pages[near >> a.page_shift]), 0), a.pages - 1);
-      const int row = (kv << a.page_shift) + (near & page_mask & ~15);
-      rows = page * a.page_bytes + static_cast<int64_t>(row) * W::kRow;
-      scales = page * a.scale_page_bytes + static_cast<int64_t>(row) * W::kScaleRow;
-    };
     auto token = [&](int tile) { return sp.base + (tile - unit_begin) * W::kTile + wave * W::kSub; };
-    int64_t row_at[W::kHalves], scale_at[W::kHalves], next_row[W::kHalves], next_scale[W::kHalves];
-    int t0 = token(first);
-    const bool any = t0 < len;
-    if (any) {
+    // A half of 16 tokens that begins at token t lies in one page.  A half without tokens takes the nearest one that has some, and is masked.
+    auto near = [&](int t) { return min(max(t, lo), len - 1); };
+    auto page_of = [&](int t) { return pages[near(t) >> a.page_shift]; };
+    auto row_of = [&](int t, int page, int64_t& rows, int64_t& scales) {
+      const int row = (kv << a.page_shift) + (near(t) & page_mask & ~15);
+      const int64_t p = min(max(page, 0), a.pages - 1);
+      rows = p * a.page_bytes + static_cast<int64_t>(row) * W::kRow;
+      scales = p * a.scale_page_bytes + static_cast<int64_t>(row) * W::kScaleRow;
+    };
+    // how many of the piece's tiles have tokens for this wave (all but the last one do)
+    const int tiles = last - first - (token(last - 1) >= len ? 1 : 0);
+    if (tiles > 0) {
+      int t0 = token(first);
+      int page[W::kHalves];                            // of the tokens whose loads are issued next, requested one round ahead
+      int64_t row[W::kHalves], scale[W::kHalves];
 #pragma unroll
       for (int h = 0; h < W::kHalves; ++h) {
-        place(t0 + 16 * h, row_at[h], scale_at[h]);
-        w.load_k(h, a.k + row_at[h], a.ks + scale_at[h], n, c);
-        w.load_v(h, a.v + row_at[h], a.vs + scale_at[h], n, c);
+        row_of(t0 + 16 * h, page_of(t0 + 16 * h), row[h], scale[h]);
+        w.load_k(h, a.k + row[h], a.ks + scale[h], n, c);
       }
-      for (int tile = first;;) {
-        const int t1 = token(tile + 1);
-        const bool more = tile + 1 < last && t1 < len;
-        if (more) {
 #pragma unroll
-          for (int h = 0; h < W::kHalves; ++h) place(t1 + 16 * h, next_row[h], next_scale[h]);
-        }
+      for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
+#pragma unroll
+      for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + W::kTile + 16 * h);
+      // one round: scores, softmax and output of the tokens in registers, and, where more follow, their loads in between.  The loads stand in
+      // straight-line code (the last round has a copy of its own): a wait for the older ones then leaves the younger ones in flight.
+      auto round = [&](auto more) {
         f32x4 s[W::kHalves];
         w.scores(s, c);
-        if (more) {
+        if constexpr (more) {
 #pragma unroll
-          for (int h = 0; h < W::kHalves; ++h) w.load_k(h, a.k + next_row[h], a.ks + next_scale[h], n, c);
+          for (int h = 0; h < W::kHalves; ++h) {
+            row_of(t0 + W::kTile + 16 * h, page[h], row[h], scale[h]);
+            w.load_k(h, a.k + row[h], a.ks + scale[h], n, c);
+          }
+#pragma unroll
+          for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kTile + 16 * h);
         }
         const bool whole = t0 >= lo && t0 + W::kSub <= len;
         uint32_t mask = 0xFFu;
@@ -408,12 +421,14 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
         }
         w.softmax(s);
         if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
-        if (!more) break;
+        if constexpr (more) {
 #pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + next_row[h], a.vs + next_scale[h], n, c);
-        ++tile;
-        t0 = t1;
-      }
+          for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
+          t0 += W::kTile;
+        }
+      };
+      for (int i = 1; i < tiles; ++i) round(std::true_type{});
+      round(std::false_type{});
     }
 
     // the four waves' parts, and out

@@ -34,8 +34,8 @@ constexpr int kMaxBlocksX = 1 << 20;                   // a workgroup walks on w
 template <class E> struct Eight;
 template <> struct Eight<bf16_t> {
   u32x4 w;
-  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
-  __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<u32x4*>(p) = w; }
+  __device__ __forceinline__ void load(const bf16_t* p) { w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+  __device__ __forceinline__ void store(bf16_t* p) const { __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p)); }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int q = 0; q < 4; ++q) { v[2 * q] = bf16_lo(w[q]); v[2 * q + 1] = bf16_hi(w[q]); }
@@ -53,8 +53,14 @@ template <> struct Eight<bf16_t> {
 };
 template <> struct Eight<float> {
   f32x4 a, b;
-  __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const f32x4*>(p)[0]; b = reinterpret_cast<const f32x4*>(p)[1]; }
-  __device__ __forceinline__ void store(float* p) const { reinterpret_cast<f32x4*>(p)[0] = a; reinterpret_cast<f32x4*>(p)[1] = b; }
+  __device__ __forceinline__ void load(const float* p) {
+    a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+    b = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1);
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    __builtin_nontemporal_store(a, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(b, reinterpret_cast<f32x4*>(p) + 1);
+  }
   __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
     for (int q = 0; q < 4; ++q) { v[q] = a[q]; v[4 + q] = b[q]; }
@@ -173,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lane
             const uint32_t code = mx_scale_code(amax);
             const uint2 w = mx_encode8(y, mx_inverse_scale(code));
             if (slot >= 0) {
-              *reinterpret_cast<uint2*>(static_cast<uint8_t*>(base) + page * a.cache.page_stride + row * a.D + chunk * 8) = w;
+              __builtin_nontemporal_store(u32x2{w.x, w.y}, reinterpret_cast<u32x2*>(static_cast<uint8_t*>(base) + page * a.cache.page_stride + row * a.D + chunk * 8));
               if ((chunk & 3) == 0)
                 static_cast<uint8_t*>(is_v ? a.cache.v_scales : a.cache.k_scales)[page * a.cache.scale_page_stride + row * (a.D / 32) + chunk / 4] =
                     static_cast<uint8_t>(code);
@@ -235,7 +241,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
           code[u] = u32x2{0u, 0u};
           scale[u] = 0u;
           if (page >= 0) {
-            code[u] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(base) + page * a.cache.page_stride + row * D + chunk * 8);
+            code[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(base) + page * a.cache.page_stride + row * D + chunk * 8));
             scale[u] = static_cast<const uint8_t*>(is_v ? a.cache.v_scales : a.cache.k_scales)[page * a.cache.scale_page_stride + row * (D / 32) + chunk / 4];
           }
         } else {

@@ -484,25 +484,33 @@ def _heads(t, dtype, name, shape=None):
     """A [T, heads, dim] device tensor whose heads are contiguous: its pointer and the strides of tokens and heads."""
     if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.dim() != 3 or not t.is_cuda:
+    st = t.stride()
+    if len(st) != 3 or not t.is_cuda:
         raise ValueError("%s must be a [tokens, heads, dim] device tensor" % name)
-    st, sh, se = t.stride()
-    if se != 1 and t.shape[2] != 1:
+    if st[2] != 1 and t.shape[2] != 1:
         raise ValueError("%s: the elements of a head must be contiguous" % name)
     if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    return t.data_ptr(), st, sh
+    return t.data_ptr(), st[0], st[1]
+
+
+_NO_HEADS = (None, 0, 0)
 
 
 def _table(cos, sin, positions, T):
-    """rot, n_pos and the pointers of a rotation's table and positions; cos None: no rotation."""
+    """The pointers of positions and a rotation's table, its n_pos and rot; cos None: no rotation."""
     if cos is None:
-        return 0, 0, None, None, None
-    _need(cos, torch.float32, "cos"); _need(sin, torch.float32, "sin"); _need(positions, torch.int32, "positions")
-    if cos.dim() != 2 or cos.shape != sin.shape or positions.numel() != T:
-        raise ValueError("cos and sin must be [n_pos, rot / 2] and positions [%d], got %s, %s and %s"
-                         % (T, tuple(cos.shape), tuple(sin.shape), tuple(positions.shape)))
-    return 2 * cos.shape[1], cos.shape[0], positions.data_ptr(), cos.data_ptr(), sin.data_ptr()
+        return None, None, None, 0, 0
+    n = cos.stride()
+    shape = cos.shape
+    if not (len(n) == 2 and n[1] == 1 and n[0] == shape[1] and sin.stride() == n and sin.shape == shape and positions.numel() == T):
+        raise ValueError("cos and sin must be [n_pos, rot / 2], contiguous, and positions [%d], got %s, %s and %s"
+                         % (T, tuple(shape), tuple(sin.shape), tuple(positions.shape)))
+    if cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or positions.dtype is not torch.int32:
+        raise TypeError("cos and sin must be float32 and positions int32, got %s, %s and %s" % (cos.dtype, sin.dtype, positions.dtype))
+    if not (cos.is_cuda and sin.is_cuda and positions.is_cuda and positions.is_contiguous()):
+        raise ValueError("cos, sin and positions must be contiguous device tensors")
+    return positions.data_ptr(), cos.data_ptr(), sin.data_ptr(), shape[0], 2 * shape[1]
 
 
 def moe_rope_table(freq, n_pos, amplitude=1.0, out=None):
@@ -520,24 +528,23 @@ def moe_rope_table(freq, n_pos, amplitude=1.0, out=None):
 
 def _rope(call, q, k, positions, cos, sin, interleaved, out):
     some = q if q is not None else k
-    T, _, D = some.shape
-    code, dtype = _dtype_code(some), some.dtype
+    dtype, (T, _, D) = some.dtype, some.shape
     if out is None:
         out = tuple(None if t is None else torch.empty(t.shape, dtype=dtype, device=some.device) for t in (q, k))
-    args, heads = [], []
-    for t, o, name in ((q, out[0], "q"), (k, out[1], "k")):
-        if t is None:
-            args.append(((None, 0, 0), (None, 0, 0)))
-            heads.append(0)
-            continue
-        shape = t.shape
+    qi = qo = ki = ko = _NO_HEADS
+    Hq = Hk = 0
+    if q is not None:
+        shape = q.shape
+        Hq = shape[1]
+        qi, qo = _heads(q, dtype, "q"), _heads(out[0], dtype, "q out", shape)
+    if k is not None:
+        shape = k.shape
+        Hk = shape[1]
         if shape[0] != T or shape[2] != D:
             raise ValueError("q and k must have the same tokens and head size")
-        args.append((_heads(t, dtype, name), _heads(o, dtype, name + " out", shape)))
-        heads.append(shape[1])
-    rot, n_pos, p_pos, p_cos, p_sin = _table(cos, sin, positions, T)
-    (qi, qo), (ki, ko) = args
-    _check(call(*qi, *ki, code, T, heads[0], heads[1], D, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, *ko, _stream()))
+        ki, ko = _heads(k, dtype, "k"), _heads(out[1], dtype, "k out", shape)
+    p_pos, p_cos, p_sin, n_pos, rot = _table(cos, sin, positions, T)
+    _check(call(*qi, *ki, _dtype_code(some), T, Hq, Hk, D, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, *ko, _stream()))
     return out
 
 
@@ -592,13 +599,14 @@ def moe_kv_cache_write(cache, k, v, slots, q=None, positions=None, cos=None, sin
     _need(slots, torch.int64, "slots")
     if slots.numel() != T:
         raise ValueError("slots must be [%d]" % T)
-    qi, qo, Hq = (None, 0, 0), (None, 0, 0), 0
+    qi = qo = _NO_HEADS
+    Hq = 0
     if q is not None:
         Hq = q.shape[1]
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=dt, device=q.device)
         qi, qo = _heads(q, dt, "q", (T, Hq, cache.dim)), _heads(q_out, dt, "q_out", q.shape)
-    rot, n_pos, p_pos, p_cos, p_sin = _table(cos, sin, positions, T)
+    p_pos, p_cos, p_sin, n_pos, rot = _table(cos, sin, positions, T)
     _check(lib.moe_kv_cache_write(cache.ref, *ki, *vi, T, slots.data_ptr(), *qi, Hq, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, _stream()))
     return q_out
 
