@@ -278,10 +278,6 @@ template <int KIND, int D> struct Wave {
   }
 };
 
-// Integers that no launch of the call writes, read by scalar loads (a vector load among those of the cache would have to be waited for with them).
-typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
-__device__ __forceinline__ ScalarInts scalar_ints(const int32_t* p) { return reinterpret_cast<ScalarInts>(reinterpret_cast<uintptr_t>(p)); }
-
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int KIND, int D>

@@ -91,6 +91,11 @@ __device__ __forceinline__ int wave_sum_i(int v) {
   return v;
 }
 
+// Integers that no launch of the call writes, the same for all lanes: read by scalar loads (a vector load among those of a stream of data
+// would have to be waited for with them).
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar_ints(const int32_t* p) { return reinterpret_cast<ScalarInts>(reinterpret_cast<uintptr_t>(p)); }
+
 // ---- row tiles of expert-ordered rows ------------------------------------------------------
 // Inclusive prefix sum over the 64 lanes: shifts inside each row of 16 lanes, then the row totals are passed on.
 __device__ __forceinline__ int wave_inclusive_sum(int v) {
