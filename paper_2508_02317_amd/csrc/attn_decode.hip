@@ -149,7 +149,7 @@ template <int KIND, int D> struct Wave {
     const uint32_t off = n * kRow + c * 16;
 #pragma unroll
     for (int i = 0; i < kKPieces; ++i) {
-      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + off + i * kKStep));
+      const u32x4 x = *reinterpret_cast<const u32x4*>(base + off + i * kKStep);
 #pragma unroll
       for (int j = 0; j < 4; ++j) k[a][i][j] = x[j];
     }
@@ -287,46 +287,45 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
   constexpr int kPad = D + 4;
   __shared__ float s_out[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  __shared__ int s_scan[kWaves + 4];
   const int lane = static_cast<int>(threadIdx.x) & 63, wave = uniform(static_cast<int>(threadIdx.x) >> 6), n = lane & 15, c = lane >> 4;
   const int units = a.Hkv * a.parts, W_ = static_cast<int>(gridDim.x), me = static_cast<int>(blockIdx.x);
   const int held = a.max_pages << a.page_shift;
 
-  // tiles of all sequences, and the sequence in which this workgroup's piece begins
-  auto span = [&](int b) { return attn_span(a.lens[b], held, a.window, W::kSub, W::kTile); };
+  // Tiles of all sequences, and the sequence in which this workgroup's piece begins.  Every wave finds them for itself, four consecutive
+  // sequences a lane, without a barrier: a load, a scan over the lanes, a ballot.
   const ScalarInts lens = scalar_ints(a.lens);
   auto span_of = [&](int b) { return attn_span(lens[b], held, a.window, W::kSub, W::kTile); };   // b the same in all lanes
+  int nt[4], mine = 0, incl = 0;                       // of this lane's sequences: tiles of each, their sum, the sum up to and with this lane
+  auto count_from = [&](int b0) {
+    mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int b = b0 + 4 * lane + j;
+      nt[j] = attn_span(b < a.B ? a.lens[b] : 0, held, a.window, W::kSub, W::kTile).tiles;
+      mine += nt[j];
+    }
+    incl = wave_inclusive_sum(mine);
+    return __builtin_amdgcn_readlane(incl, 63);
+  };
   int total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + static_cast<int>(threadIdx.x);
-    const int nt = b < a.B ? span(b).tiles : 0;
-    const int s = wave_sum_i(nt);
-    __syncthreads();
-    if (lane == 0) s_scan[wave] = s;
-    __syncthreads();
-    total += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
-  }
-  total = uniform(total) * units;
-  const AttnCut cut = attn_cut(total, W_);
+  for (int b0 = 0; b0 < a.B; b0 += 256) total += count_from(b0);
+  const AttnCut cut = attn_cut(total * units, W_);
   int at = attn_begin(cut, me);
   const int end = attn_begin(cut, me + 1);
   int b_at = 0, before = 0;                            // sequence of tile `at`, tiles (of one unit) of the sequences before it
   if (at < end) {
-    int run = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-      const int b = b0 + static_cast<int>(threadIdx.x);
-      const int nt = b < a.B ? span(b).tiles : 0;
-      const int incl = wave_inclusive_sum(nt);
-      __syncthreads();
-      if (lane == 63) s_scan[wave] = incl;
-      if (threadIdx.x == 0) s_scan[4] = -1;
-      __syncthreads();
-      int ahead = run + incl - nt;
-      for (int w = 0; w < wave; ++w) ahead += s_scan[w];
-      if (nt > 0 && ahead * units <= at && at < (ahead + nt) * units) { s_scan[4] = b; s_scan[5] = ahead; }
-      __syncthreads();
-      if (s_scan[4] >= 0) { b_at = uniform(s_scan[4]); before = uniform(s_scan[5]); break; }
-      run += s_scan[0] + s_scan[1] + s_scan[2] + s_scan[3];
+    for (int b0 = 0;; b0 += 256) {
+      const int here = a.B > 256 ? count_from(b0) : total;
+      if (at >= (before + here) * units) { before += here; continue; }
+      const int l = __builtin_ctzll(__ballot((before + incl) * units > at));   // the first lane whose sequences end behind the tile
+      before += __builtin_amdgcn_readlane(incl - mine, l);
+      b_at = b0 + 4 * l;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        const int n_j = __builtin_amdgcn_readlane(nt[j], l);
+        if (b_at == b0 + 4 * l + j && at >= (before + n_j) * units) { before += n_j; ++b_at; }
+      }
+      break;
     }
   }
 
@@ -485,54 +484,66 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
 }
 
 // ---- pieces of a context joined: a workgroup per sequence and head ---------------------------------------
+// A slice of lanes takes every kSlices-th piece, maximum, sum and output at once and kAhead pieces in flight; the slices meet in LDS.
 template <int KIND, int D>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a) {
   typedef std::conditional_t<KIND == MOE_F32, float, bf16_t> E;
-  constexpr int kCols = D / 4, kSlices = kThreads / kCols;
-  __shared__ float s_f[kAttnMaxBlocks + 1];
-  __shared__ float s_red[2 * kWaves];
+  constexpr int kCols = D / 4, kSlices = kThreads / kCols, kAhead = 4;
+  __shared__ float s_m[kSlices], s_l[kSlices];
   __shared__ float s_out[kSlices][D];
-  const int units = a.Hkv * a.parts, tid = static_cast<int>(threadIdx.x), lane = tid & 63, wave = tid >> 6;
+  const int units = a.Hkv * a.parts, tid = static_cast<int>(threadIdx.x);
   const int b = blockIdx.x / a.Hq, head = blockIdx.x - b * a.Hq, kv = head / a.group, in_group = head - kv * a.group;
   const int part = in_group / a.heads, h = in_group - part * a.heads;
-  const int32_t* p = a.unit_pieces + 2 * (static_cast<int64_t>(b) * units + kv * a.parts + part);
-  const int slot0 = p[0];
+  const ScalarInts p = scalar_ints(a.unit_pieces + 2 * (static_cast<int64_t>(b) * units + kv * a.parts + part));
+  const int slot0 = p[0], w0 = slot0 >> 1, count = p[1] - w0 + 1;
   if (slot0 < 0) return;
-  const int w0 = slot0 >> 1, count = min(p[1] - w0 + 1, kAttnMaxBlocks);
-  // the first piece may be its workgroup's second; all others are their workgroup's first
-  auto piece = [&](int i) { return a.slots + (static_cast<int64_t>(i == 0 ? slot0 : 2 * (w0 + i)) * a.heads + h) * (D + 4); };
-  float top = -INFINITY;
-  for (int i = tid; i < count; i += kThreads) {
-    s_f[i] = piece(i)[0];
-    top = fmaxf(top, s_f[i]);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  if (lane == 0) s_red[wave] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-  float sum = 0.0f;
-  for (int i = tid; i < count; i += kThreads) {
-    const float m = s_f[i], f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
-    sum += piece(i)[1] * f;
-    s_f[i] = f;
-  }
-  sum = wave_sum(sum);
-  if (lane == 0) s_red[kWaves + wave] = sum;
-  __syncthreads();
-  sum = (s_red[kWaves] + s_red[kWaves + 1]) + (s_red[kWaves + 2] + s_red[kWaves + 3]);
   const int slice = tid / kCols, d = (tid - slice * kCols) * 4;
   if (slice < kSlices) {
+    float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int i = slice; i < count; i += kSlices) o += *reinterpret_cast<const f32x4*>(piece(i) + 4 + d) * s_f[i];
+    for (int i0 = slice; i0 < count; i0 += kAhead * kSlices) {
+      float mi[kAhead], li[kAhead];
+      f32x4 oi[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = min(i0 + j * kSlices, count - 1);
+        // the first piece may be its workgroup's second; all others are their workgroup's first
+        const float* at = a.slots + (static_cast<int64_t>(i == 0 ? slot0 : 2 * (w0 + i)) * a.heads + h) * (D + 4);
+        mi[j] = at[0];
+        li[j] = at[1];
+        oi[j] = *reinterpret_cast<const f32x4*>(at + 4 + d);
+      }
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) top = i0 + j * kSlices < count ? fmaxf(top, mi[j]) : top;
+      const float base = top > -INFINITY ? top : 0.0f;   // a maximum of -inf counts with weight 0
+      const float f = __builtin_amdgcn_exp2f(m - base);
+      l *= f;
+      o *= f;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const float g = i0 + j * kSlices < count ? __builtin_amdgcn_exp2f(mi[j] - base) : 0.0f;
+        l += li[j] * g;
+        o += oi[j] * g;
+      }
+      m = top;
+    }
+    if (d == 0) { s_m[slice] = m; s_l[slice] = l; }
     *reinterpret_cast<f32x4*>(&s_out[slice][d]) = o;
   }
   __syncthreads();
   if (tid < kCols) {
+    float top = s_m[0], sum = 0.0f;
+#pragma unroll
+    for (int s = 1; s < kSlices; ++s) top = fmaxf(top, s_m[s]);
+    const float base = top > -INFINITY ? top : 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int s = 0; s < kSlices; ++s) o += *reinterpret_cast<const f32x4*>(&s_out[s][d]);
+    for (int s = 0; s < kSlices; ++s) {
+      const float f = __builtin_amdgcn_exp2f(s_m[s] - base);
+      sum += s_l[s] * f;
+      o += *reinterpret_cast<const f32x4*>(&s_out[s][d]) * f;
+    }
     const int64_t row = static_cast<int64_t>(b) * a.Hq + head;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     if constexpr (KIND == MOE_F32) {
