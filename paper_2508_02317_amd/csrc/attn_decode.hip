@@ -54,7 +54,7 @@ struct Args {
   const int32_t *block_table, *lens;
   int max_pages, B, Hq, Hkv, group, parts, heads;      // group: query heads per key head, in `parts` units of up to `heads`
   float scale_log2;
-  int window;
+  int window, tile_subs;                              // tile_subs: stretches of kSub tokens in a tile, four of them or a whole context
   void* out;
   float* lse;
   int32_t* unit_pieces;                                // [B * Hkv * parts][2]: first workgroup (its slot in bit 0) and last of a cut unit, or -1
@@ -100,7 +100,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // What a wave holds of its tokens, and the products with it.
 template <int KIND, int D> struct Wave {
   static constexpr bool kF32 = KIND == MOE_F32, kMx = KIND == MOE_MX8;
-  static constexpr int kHalves = kF32 ? 1 : 2, kSub = 16 * kHalves, kTile = kWaves * kSub;
+  static constexpr int kHalves = kF32 ? 1 : 2, kSub = 16 * kHalves, kStep = kWaves * kSub;   // tokens of a wave, of a workgroup at a time
   static constexpr int kG = D % 128 == 0 ? 128 : 64, kE = kG / 16, kNG = D / kG;   // a lane's values: kE elements of each of kNG groups of kG
   static constexpr int kEs = kF32 ? 4 : kMx ? 1 : 2, kRow = D * kEs;               // bytes of an element, of a token's row
   static constexpr int kKPieces = kMx ? D / 64 : kF32 ? D / 16 : D / 32;           // 16-byte pieces of a key row that a lane reads
@@ -281,27 +281,32 @@ template <int KIND, int D> struct Wave {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int KIND, int D>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_kernel(Args a) {
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(Args a) {
   typedef Wave<KIND, D> W;
   typedef std::conditional_t<KIND == MOE_F32, float, bf16_t> E;
   constexpr int kPad = D + 4;
   __shared__ float s_out[kWaves][16][kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   const int lane = static_cast<int>(threadIdx.x) & 63, wave = uniform(static_cast<int>(threadIdx.x) >> 6), n = lane & 15, c = lane >> 4;
-  const int units = a.Hkv * a.parts, W_ = static_cast<int>(gridDim.x), me = static_cast<int>(blockIdx.x);
+  const int units = a.Hkv * a.parts, me = static_cast<int>(blockIdx.x);
   const int held = a.max_pages << a.page_shift;
 
   // Tiles of all sequences, and the sequence in which this workgroup's piece begins.  Every wave finds them for itself, four consecutive
   // sequences a lane, without a barrier: a load, a scan over the lanes, a ballot.
   const ScalarInts lens = scalar_ints(a.lens);
-  auto span_of = [&](int b) { return attn_span(lens[b], held, a.window, W::kSub, W::kTile); };   // b the same in all lanes
-  int nt[4], mine = 0, incl = 0;                       // of this lane's sequences: tiles of each, their sum, the sum up to and with this lane
+  const int tile = a.tile_subs * W::kSub;
+  auto span_of = [&](int len) { return attn_span(len, held, a.window, W::kSub, tile); };
+  int len4[4], nt[4], mine = 0, incl = 0;              // of this lane's sequences: lengths, tiles of each, their sum, the sum up to and with this lane
   auto count_from = [&](int b0) {
     mine = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int b = b0 + 4 * lane + j;
-      nt[j] = attn_span(b < a.B ? a.lens[b] : 0, held, a.window, W::kSub, W::kTile).tiles;
+      len4[j] = b < a.B ? a.lens[b] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      nt[j] = span_of(len4[j]).tiles;
       mine += nt[j];
     }
     incl = wave_inclusive_sum(mine);
@@ -309,10 +314,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
   };
   int total = 0;
   for (int b0 = 0; b0 < a.B; b0 += 256) total += count_from(b0);
-  const AttnCut cut = attn_cut(total * units, W_);
+  const AttnCut cut = attn_cut(total * units, static_cast<int>(gridDim.x));
   int at = attn_begin(cut, me);
   const int end = attn_begin(cut, me + 1);
-  int b_at = 0, before = 0;                            // sequence of tile `at`, tiles (of one unit) of the sequences before it
+  int b_at = 0, before = 0, len_at = 0;                // sequence of tile `at`, tiles (of one unit) of the sequences before it, its length
   if (at < end) {
     for (int b0 = 0;; b0 += 256) {
       const int here = a.B > 256 ? count_from(b0) : total;
@@ -320,18 +325,23 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
       const int l = __builtin_ctzll(__ballot((before + incl) * units > at));   // the first lane whose sequences end behind the tile
       before += __builtin_amdgcn_readlane(incl - mine, l);
       b_at = b0 + 4 * l;
+      len_at = __builtin_amdgcn_readlane(len4[0], l);
 #pragma unroll
       for (int j = 0; j < 3; ++j) {
         const int n_j = __builtin_amdgcn_readlane(nt[j], l);
-        if (b_at == b0 + 4 * l + j && at >= (before + n_j) * units) { before += n_j; ++b_at; }
+        if (b_at == b0 + 4 * l + j && at >= (before + n_j) * units) {
+          before += n_j;
+          ++b_at;
+          len_at = __builtin_amdgcn_readlane(len4[j + 1], l);
+        }
       }
       break;
     }
   }
 
   // sequences without tokens
-  for (int b = me; b < a.B; b += W_) {
-    if (span_of(b).tiles != 0) continue;
+  for (int b = me; b < a.B; b += static_cast<int>(gridDim.x)) {
+    if (span_of(lens[b]).tiles != 0) continue;
     for (int i = threadIdx.x; i < a.Hq * D; i += kThreads) static_cast<E*>(a.out)[static_cast<int64_t>(b) * a.Hq * D + i] = 0;
     if (a.lse)
       for (int i = threadIdx.x; i < a.Hq; i += kThreads) a.lse[static_cast<int64_t>(b) * a.Hq + i] = -INFINITY;
@@ -339,18 +349,19 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
       for (int i = threadIdx.x; i < units; i += kThreads) a.unit_pieces[2 * (static_cast<int64_t>(b) * units + i)] = -1;
   }
 
-  W w;
   while (at < end) {
-    AttnSpan sp = span_of(b_at);
+    AttnSpan sp = span_of(len_at);
     while (at >= (before + sp.tiles) * units) {        // on to the sequence that has the tile
       before += sp.tiles;
-      sp = span_of(++b_at);
+      len_at = lens[++b_at];
+      sp = span_of(len_at);
     }
     const int u = (at - before * units) / sp.tiles, unit_begin = before * units + u * sp.tiles, unit_end = unit_begin + sp.tiles;
     const int first = at, last = min(end, unit_end);
     const int kv = u / a.parts, part = u - kv * a.parts, head0 = kv * a.group + part * a.heads, heads = min(a.heads, a.group - part * a.heads);
     const int lo = sp.lo, len = sp.len;
 
+    W w;
     {
       const int h = head0 + min(n, heads - 1);         // columns without a head repeat the last one's
       w.load_q(static_cast<const char*>(a.q) + (static_cast<int64_t>(b_at) * a.q_stride_b + static_cast<int64_t>(h) * a.q_stride_h) * static_cast<int>(sizeof(E)), c);
@@ -358,7 +369,6 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
     w.begin();
     const ScalarInts pages = scalar_ints(a.block_table + static_cast<int64_t>(b_at) * a.max_pages);
     const int page_mask = (1 << a.page_shift) - 1;
-    auto token = [&](int tile) { return sp.base + (tile - unit_begin) * W::kTile + wave * W::kSub; };
     // A half of 16 tokens that begins at token t lies in one page.  A half without tokens takes the nearest one that has some, and is masked.
     auto near = [&](int t) { return min(max(t, lo), len - 1); };
     auto page_of = [&](int t) { return pages[near(t) >> a.page_shift]; };
@@ -368,10 +378,11 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
       rows = p * a.page_bytes + static_cast<int64_t>(row) * W::kRow;
       scales = p * a.scale_page_bytes + static_cast<int64_t>(row) * W::kScaleRow;
     };
-    // how many of the piece's tiles have tokens for this wave (all but the last one do)
-    const int tiles = last - first - (token(last - 1) >= len ? 1 : 0);
-    if (tiles > 0) {
-      int t0 = token(first);
+    // the wave takes every fourth of the piece's stretches of kSub tokens
+    const int sub0 = (first - unit_begin) * a.tile_subs + wave, sub1 = min((last - unit_begin) * a.tile_subs, (len - sp.base + W::kSub - 1) / W::kSub);
+    const int rounds = (sub1 - sub0 + kWaves - 1) / kWaves;
+    if (sub0 < sub1) {
+      int t0 = sp.base + sub0 * W::kSub;
       int page[W::kHalves];                            // of the tokens whose loads are issued next, requested one round ahead
       int64_t row[W::kHalves], scale[W::kHalves];
 #pragma unroll
@@ -382,21 +393,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
 #pragma unroll
       for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
 #pragma unroll
-      for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + W::kTile + 16 * h);
-      // one round: scores, softmax and output of the tokens in registers, and, where more follow, their loads in between.  The loads stand in
-      // straight-line code (the last round has a copy of its own): a wait for the older ones then leaves the younger ones in flight.
-      auto round = [&](auto more) {
-        f32x4 s[W::kHalves];
-        w.scores(s, c);
-        if constexpr (more) {
-#pragma unroll
-          for (int h = 0; h < W::kHalves; ++h) {
-            row_of(t0 + W::kTile + 16 * h, page[h], row[h], scale[h]);
-            w.load_k(h, a.k + row[h], a.ks + scale[h], n, c);
-          }
-#pragma unroll
-          for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kTile + 16 * h);
-        }
+      for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + W::kStep + 16 * h);
+      // What follows the scores of the tokens in registers.
+      f32x4 s[W::kHalves];
+      auto rest = [&]() {
         const bool whole = t0 >= lo && t0 + W::kSub <= len;
         uint32_t mask = 0xFFu;
         if (whole) {
@@ -416,14 +416,26 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : ATT_OCC) void attn_decode_k
         }
         w.softmax(s);
         if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
-        if constexpr (more) {
-#pragma unroll
-          for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
-          t0 += W::kTile;
-        }
       };
-      for (int i = 1; i < tiles; ++i) round(std::true_type{});
-      round(std::false_type{});
+      // Where more tokens follow, their keys are requested as soon as the scores are formed and their values after the output.  The requests
+      // stand in straight-line code (the last tokens have a copy of the rest of their own): a wait for the older ones then leaves the younger ones
+      // in flight.  They stay behind the reads of the registers they go to, so that one set of registers serves.
+      for (int i = 1;; ++i) {
+        w.scores(s, c);
+        if (i >= rounds) break;
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) {
+          row_of(t0 + W::kStep + 16 * h, page[h], row[h], scale[h]);
+          w.load_k(h, a.k + row[h], a.ks + scale[h], n, c);
+        }
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kStep + 16 * h);
+        rest();
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
+        t0 += W::kStep;
+      }
+      rest();
     }
 
     // the four waves' parts, and out
@@ -556,19 +568,24 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a) {
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
-// Tiles of a context of the whole page table, and the grid: never more workgroups than tiles, nor than kAttnMaxBlocks.
-struct Launch { int tile, parts, heads, blocks; int64_t most_tiles; bool cut; };
-Launch launch_of(int dtype, int B, int Hq, int Hkv, int page_size, int max_pages) {
+struct Launch { int sub, tile_subs, parts, heads, blocks; int64_t most_subs; bool cut; };
+Launch launch_of(int dtype, int B, int Hq, int Hkv, int page_size, int max_pages, int window) {
   Launch l;
-  l.tile = kWaves * (dtype == MOE_F32 ? 16 : 32);
+  l.sub = dtype == MOE_F32 ? 16 : 32;
   const int group = Hq / Hkv;
   l.parts = ceil_div(group, 16);
   l.heads = ceil_div(group, l.parts);
-  const int64_t held = static_cast<int64_t>(page_size) * max_pages, tiles = (held + l.tile - 1) / l.tile + 1;   // a window may begin inside a tile
-  l.most_tiles = tiles * B * Hkv * l.parts;
-  l.blocks = static_cast<int>(l.most_tiles < kAttnMaxBlocks ? l.most_tiles : kAttnMaxBlocks);
+  const int64_t units = static_cast<int64_t>(B) * Hkv * l.parts, held = static_cast<int64_t>(page_size) * max_pages;
+  const int64_t seen = window > 0 && window + l.sub < held ? window + l.sub : held, subs = (seen + l.sub - 1) / l.sub;   // a window may begin inside a stretch
+  // A context of few stretches is not cut (its one tile is the whole): a workgroup has it in a few turns, and no second launch is needed.
+  // 4 key heads of 128 elements in bf16, cut -> whole: one context of 250 tokens 11.1 -> 7.9 us, 500 10.8 -> 9.5, 1000 10.8 -> 14.4; 64 contexts of
+  // 250 14.4 -> 10.2, 500 18.4 -> 14.6, 1000 27.2 -> 23.6; 512 of 250 63 -> 54, 1000 180 -> 173.
+  l.cut = subs > (units >= 256 ? 32 : 16);
+  l.tile_subs = l.cut ? kWaves : static_cast<int>(subs < 1 ? 1 : subs);
+  l.most_subs = subs * units;
+  const int64_t most = (l.cut ? (subs + kWaves - 1) / kWaves : 1) * units;
+  l.blocks = static_cast<int>(most < kAttnMaxBlocks ? most : kAttnMaxBlocks);
   if (l.blocks < 1) l.blocks = 1;
-  l.cut = held > l.tile;
   return l;
 }
 // the larger of the element types' workspaces: the query does not know the cache's type
@@ -596,8 +613,8 @@ using namespace moe;
 
 extern "C" size_t moe_paged_attn_decode_workspace_bytes(int B, int Hq, int heads, int dim, int page_size, int max_pages) {
   if (B <= 0 || Hq <= 0 || heads <= 0 || dim <= 0 || page_size <= 0 || max_pages <= 0 || Hq % heads != 0) return 256;
-  const size_t f32 = ws_bytes_of(launch_of(MOE_F32, B, Hq, heads, page_size, max_pages), B, heads, dim);
-  const size_t bf16 = ws_bytes_of(launch_of(MOE_BF16, B, Hq, heads, page_size, max_pages), B, heads, dim);
+  const size_t f32 = ws_bytes_of(launch_of(MOE_F32, B, Hq, heads, page_size, max_pages, 0), B, heads, dim);
+  const size_t bf16 = ws_bytes_of(launch_of(MOE_BF16, B, Hq, heads, page_size, max_pages, 0), B, heads, dim);
   return f32 > bf16 ? f32 : bf16;
 }
 
@@ -617,8 +634,8 @@ extern "C" int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int6
   MOE_REQUIRE(static_cast<int64_t>(cache->page_size) * max_pages < (int64_t{1} << 31) - 4096, MOE_ERR_UNSUPPORTED, "paged_attn_decode: contexts of %lld tokens",
               static_cast<long long>(cache->page_size) * max_pages);
   MOE_REQUIRE(static_cast<int64_t>(B) * Hq <= (1 << 23), MOE_ERR_UNSUPPORTED, "paged_attn_decode: B * Hq = %lld above 2^23", static_cast<long long>(B) * Hq);
-  const Launch l = launch_of(cache->dtype, B, Hq, cache->heads, cache->page_size, max_pages);
-  MOE_REQUIRE(l.most_tiles < (int64_t{1} << 31) - 65536, MOE_ERR_UNSUPPORTED, "paged_attn_decode: %lld tiles of %d tokens", static_cast<long long>(l.most_tiles), l.tile);
+  const Launch l = launch_of(cache->dtype, B, Hq, cache->heads, cache->page_size, max_pages, window);
+  MOE_REQUIRE(l.most_subs < (int64_t{1} << 31) - 65536, MOE_ERR_UNSUPPORTED, "paged_attn_decode: %lld stretches of %d tokens", static_cast<long long>(l.most_subs), l.sub);
   const size_t need = moe_paged_attn_decode_workspace_bytes(B, Hq, cache->heads, cache->dim, cache->page_size, max_pages);
   MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "paged_attn_decode: workspace null, misaligned or smaller than %zu bytes", need);
   Args a{};
@@ -629,7 +646,7 @@ extern "C" int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int6
   a.scale_page_bytes = cache->scale_page_stride;
   a.pages = cache->pages; a.page_shift = __builtin_ctz(cache->page_size);
   a.block_table = block_table; a.lens = lens; a.max_pages = max_pages; a.B = B; a.Hq = Hq; a.Hkv = cache->heads; a.group = Hq / cache->heads;
-  a.parts = l.parts; a.heads = l.heads; a.scale_log2 = scale * kLog2e; a.window = window; a.out = out; a.lse = lse;
+  a.parts = l.parts; a.heads = l.heads; a.scale_log2 = scale * kLog2e; a.window = window; a.tile_subs = l.tile_subs; a.out = out; a.lse = lse;
   if (l.cut) {
     a.unit_pieces = static_cast<int32_t*>(ws);
     a.slots = reinterpret_cast<float*>(static_cast<char*>(ws) + pieces_bytes(B, cache->heads, l.parts));

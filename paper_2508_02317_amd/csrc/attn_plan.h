@@ -5,11 +5,7 @@
 
 namespace moe {
 
-#ifndef ATT_BLOCKS
-#define ATT_BLOCKS 512
-#define ATT_OCC 2
-#endif
-constexpr int kAttnMaxBlocks = ATT_BLOCKS;                    // workgroups of a launch
+constexpr int kAttnMaxBlocks = 512;                    // workgroups of a launch
 
 // Tokens [lo, len) of a sequence are seen, in `tiles` tiles of `tile` tokens from `base` on, a multiple of `sub` at or below lo.
 struct AttnSpan { int lo, len, base, tiles; };
