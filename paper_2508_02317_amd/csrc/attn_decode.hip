@@ -41,6 +41,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x1 __attribute__((ext_vector_type(1)));
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -76,26 +77,32 @@ __device__ __forceinline__ float row_sum4(float v) {
 __device__ __forceinline__ float scale_of(uint32_t code) {   // 2^(code - 127)
   return __uint_as_float(code << 23);
 }
-// Words loaded from memory with the alignment that head rows have: whole vectors of 4, 2 or 1 words.
-template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const char* p) {
-  if constexpr (N % 4 == 0) {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
-    }
-  } else if constexpr (N % 2 == 0) {
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p) + i);
-      w[2 * i] = x[0]; w[2 * i + 1] = x[1];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p) + i);
+// 16 rows of a page as a buffer: a lane's offset is the same for all tokens, and rows that are not there (range 0) are not fetched, so that loads
+// ahead need no branch around them.
+struct Rows {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ Rows(const char* first, uint32_t range) {
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first), 0, static_cast<int>(range), 0x00020000);
   }
-}
+  // aux 2: streamed
+  template <class V, int AUX> __device__ __forceinline__ V load(uint32_t off) const {
+    if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(rsrc, static_cast<int>(off), 0, AUX));
+    else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(rsrc, static_cast<int>(off), 0, AUX));
+    else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(rsrc, static_cast<int>(off), 0, AUX));
+    else return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b16(rsrc, static_cast<int>(off), 0, AUX));
+  }
+};
+// N consecutive words in the widest vectors that divide them.
+template <int N> struct Words {
+  typedef std::conditional_t<N % 4 == 0, u32x4, std::conditional_t<N % 2 == 0, u32x2, u32x1>> V;
+  static constexpr int kLanes = sizeof(V) / 4;
+  V w[N / kLanes];
+  template <int AUX> __device__ __forceinline__ void load(const Rows& rows, uint32_t off) {
+#pragma unroll
+    for (int i = 0; i < N / kLanes; ++i) w[i] = rows.template load<V, AUX>(off + i * static_cast<int>(sizeof(V)));
+  }
+  __device__ __forceinline__ uint32_t operator[](int i) const { return w[i / kLanes][i % kLanes]; }
+};
 
 // What a wave holds of its tokens, and the products with it.
 template <int KIND, int D> struct Wave {
@@ -104,36 +111,25 @@ template <int KIND, int D> struct Wave {
   static constexpr int kG = D % 128 == 0 ? 128 : 64, kE = kG / 16, kNG = D / kG;   // a lane's values: kE elements of each of kNG groups of kG
   static constexpr int kEs = kF32 ? 4 : kMx ? 1 : 2, kRow = D * kEs;               // bytes of an element, of a token's row
   static constexpr int kKPieces = kMx ? D / 64 : kF32 ? D / 16 : D / 32;           // 16-byte pieces of a key row that a lane reads
-  static constexpr int kKStep = kMx ? 64 : kF32 ? 64 : 64;                         // bytes between them (4 lanes of 16 bytes)
+  static constexpr int kKStep = 64;                                                // bytes between them (4 lanes of 16 bytes)
   static constexpr int kVTokens = 4 * kHalves, kVWords = kE * kEs / 4;             // tokens and words of a group that a lane reads of the values
   static constexpr int kScaleRow = D / 32;                                         // scale bytes of a token
-  static constexpr int kQWords = kF32 ? D / 4 : D / 8;
+  static constexpr int kQPieces = kF32 ? D / 16 : D / 32;                          // 16-byte pieces of a query that a lane holds
 
-  uint32_t k[kHalves][kKPieces][4];
-  uint32_t v[kVTokens][kNG][kVWords];
+  u32x4 k[kHalves][kKPieces];
+  Words<kVWords> v[kVTokens][kNG];
   uint16_t ks[kMx ? kHalves : 1][kMx ? D / 64 : 1];
-  uint32_t vs[kMx ? kHalves : 1][kMx ? kScaleRow : 1];   // 4 tokens' scale bytes
-  uint32_t q[kQWords];
+  Words<kMx ? kScaleRow : 1> vs[kMx ? kHalves : 1];      // 4 tokens' scale bytes
+  u32x4 q[kQPieces];
   f32x4 acc[kNG][kE];
   float m, l;
 
   __device__ __forceinline__ void load_q(const char* head_row, int c) {
-    if constexpr (kF32) {
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(head_row + i * 64 + c * 16);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q[4 * i + j] = x[j];
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        // the elements of step s that the keys' lane holds: bf16 32 s + 8 c, 8 bits 64 (s / 2) + 16 c + 8 (s % 2)
-        const int at = kMx ? (s / 2) * 64 + c * 16 + (s % 2) * 8 : s * 32 + c * 8;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(head_row + at * 2);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q[4 * s + j] = x[j];
-      }
+    for (int i = 0; i < kQPieces; ++i) {
+      // the elements that the keys' lane holds: bytes 64 i + 16 c on, or for 8-bit keys the elements 64 (i / 2) + 16 c + 8 (i % 2) on
+      const int at = kMx ? ((i / 2) * 64 + c * 16 + (i % 2) * 8) * 2 : i * 64 + c * 16;
+      q[i] = *reinterpret_cast<const u32x4*>(head_row + at);
     }
   }
   __device__ __forceinline__ void begin() {
@@ -144,27 +140,21 @@ template <int KIND, int D> struct Wave {
 #pragma unroll
       for (int e = 0; e < kE; ++e) acc[g][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  // half a's 16 tokens begin at `base` (keys) and `sbase` (their scales); n, c: of the lane
-  __device__ __forceinline__ void load_k(int a, const char* base, const char* sbase, int n, int c) {
-    const uint32_t off = n * kRow + c * 16;
+  // half a's 16 tokens: their rows and the rows of their scales; n, c: of the lane
+  __device__ __forceinline__ void load_k(int a, const Rows& rows, const Rows& scales, int n, int c) {
 #pragma unroll
-    for (int i = 0; i < kKPieces; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(base + off + i * kKStep);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) k[a][i][j] = x[j];
-    }
+    for (int i = 0; i < kKPieces; ++i) k[a][i] = rows.template load<u32x4, 0>(n * kRow + c * 16 + i * kKStep);
     if constexpr (kMx) {
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) ks[a][i] = *reinterpret_cast<const uint16_t*>(sbase + static_cast<uint32_t>(n * kScaleRow) + 2 * i);
+      for (int i = 0; i < D / 64; ++i) ks[a][i] = scales.template load<uint16_t, 0>(n * kScaleRow + 2 * i);
     }
   }
-  __device__ __forceinline__ void load_v(int a, const char* base, const char* sbase, int n, int c) {
-    const uint32_t off = c * 4 * kRow + n * kE * kEs;
+  __device__ __forceinline__ void load_v(int a, const Rows& rows, const Rows& scales, int n, int c) {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int g = 0; g < kNG; ++g) load_words(v[4 * a + r][g], base + off + r * kRow + g * kG * kEs);
-    if constexpr (kMx) load_words(vs[a], sbase + static_cast<uint32_t>(c * 4 * kScaleRow));
+      for (int g = 0; g < kNG; ++g) v[4 * a + r][g].template load<2>(rows, c * 4 * kRow + n * kE * kEs + r * kRow + g * kG * kEs);
+    if constexpr (kMx) vs[a].template load<0>(scales, c * 4 * kScaleRow);
   }
   // eight codes (two words) -> eight bf16
   static __device__ __forceinline__ bf16x8 decode8(uint32_t w0, uint32_t w1, float s) {
@@ -181,17 +171,15 @@ template <int KIND, int D> struct Wave {
       for (int a = 0; a < kHalves; ++a) {
         if constexpr (kF32) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[4 * i + j]), s[a], 0, 0, 0);
+          for (int j = 0; j < 4; ++j) s[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[i][j]), s[a], 0, 0, 0);
         } else if constexpr (kMx) {
           const float sc = scale_of((static_cast<uint32_t>(ks[a][i]) >> (8 * (c >> 1))) & 0xFFu);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const u32x4 qq = {q[8 * i + 4 * h], q[8 * i + 4 * h + 1], q[8 * i + 4 * h + 2], q[8 * i + 4 * h + 3]};
-            s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, qq), s[a], 0, 0, 0);
+            s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, q[2 * i + h]), s[a], 0, 0, 0);
           }
         } else {
-          const u32x4 kk = {k[a][i][0], k[a][i][1], k[a][i][2], k[a][i][3]}, qq = {q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]};
-          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, qq), s[a], 0, 0, 0);
+          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[a][i]), __builtin_bit_cast(bf16x8, q[i]), s[a], 0, 0, 0);
         }
       }
   }
@@ -385,18 +373,33 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       int t0 = sp.base + sub0 * W::kSub;
       int page[W::kHalves];                            // of the tokens whose loads are issued next, requested one round ahead
       int64_t row[W::kHalves], scale[W::kHalves];
+      auto load_k = [&](bool there) {
 #pragma unroll
-      for (int h = 0; h < W::kHalves; ++h) {
-        row_of(t0 + 16 * h, page_of(t0 + 16 * h), row[h], scale[h]);
-        w.load_k(h, a.k + row[h], a.ks + scale[h], n, c);
-      }
+        for (int h = 0; h < W::kHalves; ++h)
+          w.load_k(h, Rows(a.k + row[h], there ? 16 * W::kRow : 0), Rows(a.ks + scale[h], there ? 16 * W::kScaleRow : 0), n, c);
+      };
+      auto load_v = [&](bool there) {
 #pragma unroll
-      for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
+        for (int h = 0; h < W::kHalves; ++h)
+          w.load_v(h, Rows(a.v + row[h], there ? 16 * W::kRow : 0), Rows(a.vs + scale[h], there ? 16 * W::kScaleRow : 0), n, c);
+      };
+#pragma unroll
+      for (int h = 0; h < W::kHalves; ++h) row_of(t0 + 16 * h, page_of(t0 + 16 * h), row[h], scale[h]);
+      load_k(true);
+      __builtin_amdgcn_sched_barrier(0);               // the order of the rounds: keys are the older ones when scores wait for them
+      load_v(true);
 #pragma unroll
       for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + W::kStep + 16 * h);
-      // What follows the scores of the tokens in registers.
-      f32x4 s[W::kHalves];
-      auto rest = [&]() {
+      // The next keys are requested as soon as the scores are formed, the next values after the output, in the last round with a range of
+      // nothing: without branches around the requests a wait for older ones leaves the younger ones in flight.
+      for (int i = 1; i <= rounds; ++i) {
+        f32x4 s[W::kHalves];
+        w.scores(s, c);
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) row_of(t0 + W::kStep + 16 * h, page[h], row[h], scale[h]);
+        load_k(i < rounds);
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kStep + 16 * h);
         const bool whole = t0 >= lo && t0 + W::kSub <= len;
         uint32_t mask = 0xFFu;
         if (whole) {
@@ -416,26 +419,9 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
         }
         w.softmax(s);
         if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
-      };
-      // Where more tokens follow, their keys are requested as soon as the scores are formed and their values after the output.  The requests
-      // stand in straight-line code (the last tokens have a copy of the rest of their own): a wait for the older ones then leaves the younger ones
-      // in flight.  They stay behind the reads of the registers they go to, so that one set of registers serves.
-      for (int i = 1;; ++i) {
-        w.scores(s, c);
-        if (i >= rounds) break;
-#pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) {
-          row_of(t0 + W::kStep + 16 * h, page[h], row[h], scale[h]);
-          w.load_k(h, a.k + row[h], a.ks + scale[h], n, c);
-        }
-#pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kStep + 16 * h);
-        rest();
-#pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) w.load_v(h, a.v + row[h], a.vs + scale[h], n, c);
+        load_v(i < rounds);
         t0 += W::kStep;
       }
-      rest();
     }
 
     // the four waves' parts, and out
