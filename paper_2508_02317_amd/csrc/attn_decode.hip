@@ -104,6 +104,24 @@ template <int N> struct Words {
   __device__ __forceinline__ uint32_t operator[](int i) const { return w[i / kLanes][i % kLanes]; }
 };
 
+// N bytes that begin at a multiple of N: whole words where N is one, else pairs of bytes.
+template <int N> struct ScaleRow {
+  typedef std::conditional_t<N % 4 == 0, Words<(N + 3) / 4>, uint16_t[(N + 1) / 2]> V;
+  V v;
+  __device__ __forceinline__ void load(const Rows& rows, uint32_t off) {
+    if constexpr (N % 4 == 0) {
+      v.template load<0>(rows, off);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) v[i] = rows.template load<uint16_t, 0>(off + 2 * i);
+    }
+  }
+  __device__ __forceinline__ uint32_t pair(int i) const {   // bytes 2 i and 2 i + 1
+    if constexpr (N % 4 == 0) return v[i / 2] >> (16 * (i % 2));
+    else return v[i];
+  }
+};
+
 // What a wave holds of its tokens, and the products with it.
 template <int KIND, int D> struct Wave {
   static constexpr bool kF32 = KIND == MOE_F32, kMx = KIND == MOE_MX8;
@@ -118,7 +136,7 @@ template <int KIND, int D> struct Wave {
 
   u32x4 k[kHalves][kKPieces];
   Words<kVWords> v[kVTokens][kNG];
-  uint16_t ks[kMx ? kHalves : 1][kMx ? D / 64 : 1];
+  ScaleRow<kMx ? kScaleRow : 4> ks[kMx ? kHalves : 1];  // a token's scale bytes
   Words<kMx ? kScaleRow : 1> vs[kMx ? kHalves : 1];      // 4 tokens' scale bytes
   u32x4 q[kQPieces];
   f32x4 acc[kNG][kE];
@@ -144,10 +162,7 @@ template <int KIND, int D> struct Wave {
   __device__ __forceinline__ void load_k(int a, const Rows& rows, const Rows& scales, int n, int c) {
 #pragma unroll
     for (int i = 0; i < kKPieces; ++i) k[a][i] = rows.template load<u32x4, 0>(n * kRow + c * 16 + i * kKStep);
-    if constexpr (kMx) {
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) ks[a][i] = scales.template load<uint16_t, 0>(n * kScaleRow + 2 * i);
-    }
+    if constexpr (kMx) ks[a].load(scales, n * kScaleRow);
   }
   __device__ __forceinline__ void load_v(int a, const Rows& rows, const Rows& scales, int n, int c) {
 #pragma unroll
@@ -173,7 +188,7 @@ template <int KIND, int D> struct Wave {
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[i][j]), s[a], 0, 0, 0);
         } else if constexpr (kMx) {
-          const float sc = scale_of((static_cast<uint32_t>(ks[a][i]) >> (8 * (c >> 1))) & 0xFFu);
+          const float sc = scale_of((ks[a].pair(i) >> (8 * (c >> 1))) & 0xFFu);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, q[2 * i + h]), s[a], 0, 0, 0);
