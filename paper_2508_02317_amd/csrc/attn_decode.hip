@@ -125,7 +125,7 @@ template <int N> struct ScaleRow {
 // What a wave holds of its tokens, and the products with it.
 template <int KIND, int D> struct Wave {
   static constexpr bool kF32 = KIND == MOE_F32, kMx = KIND == MOE_MX8;
-  static constexpr int kHalves = kF32 ? 1 : 2, kSub = 16 * kHalves, kStep = kWaves * kSub;   // tokens of a wave, of a workgroup at a time
+  static constexpr int kHalves = attn_halves(KIND, D), kSub = 16 * kHalves, kStep = kWaves * kSub;   // tokens of a wave, of a workgroup at a time
   static constexpr int kG = D % 128 == 0 ? 128 : 64, kE = kG / 16, kNG = D / kG;   // a lane's values: kE elements of each of kNG groups of kG
   static constexpr int kEs = kF32 ? 4 : kMx ? 1 : 2, kRow = D * kEs;               // bytes of an element, of a token's row
   static constexpr int kKPieces = kMx ? D / 64 : kF32 ? D / 16 : D / 32;           // 16-byte pieces of a key row that a lane reads
@@ -228,19 +228,21 @@ template <int KIND, int D> struct Wave {
   template <bool CUT> __device__ __forceinline__ void output(const f32x4 (&p)[kHalves], uint32_t mask, int n) {
     if constexpr (kF32) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < kVTokens; ++r)
 #pragma unroll
         for (int g = 0; g < kNG; ++g)
 #pragma unroll
           for (int e = 0; e < kE; ++e) {
             const float x = CUT && !((mask >> r) & 1u) ? 0.0f : __uint_as_float(v[r][g][e]);
-            acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[0][r], acc[g][e], 0, 0, 0);
+            acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[r / 4][r % 4], acc[g][e], 0, 0, 0);
           }
     } else {
+#pragma unroll
+     for (int two = 0; two < kHalves; two += 2) {
       u32x4 hi, lo;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {                    // tokens 16 (i / 2) + 4 c + 2 (i % 2) and the next
-        const float x = p[i / 2][2 * (i % 2)], y = p[i / 2][2 * (i % 2) + 1];
+      for (int i = 0; i < 4; ++i) {                    // tokens 16 (two + i / 2) + 4 c + 2 (i % 2) and the next
+        const float x = p[two + i / 2][2 * (i % 2)], y = p[two + i / 2][2 * (i % 2) + 1];
         hi[i] = pack_bf16x2(x, y);
         lo[i] = pack_bf16x2(x - bf16_lo(hi[i]), y - bf16_hi(hi[i]));
       }
@@ -250,21 +252,22 @@ template <int KIND, int D> struct Wave {
         uint32_t w[8][kE / 2];                         // bf16 pairs of the lane's elements, by token
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
+          const int vt = 4 * two + t;
           if constexpr (kMx) {
             const int at = (t & 3) * kScaleRow + g * (kG / 32);        // byte of the first of the row's scales for this group
-            const float sc = scale_of((vs[t >> 2][at >> 2] >> (8 * ((at & 3) + n * kE / 32))) & 0xFFu);
+            const float sc = scale_of((vs[vt >> 2][at >> 2] >> (8 * ((at & 3) + n * kE / 32))) & 0xFFu);
 #pragma unroll
             for (int e = 0; e < kE / 4; ++e) {
-              w[t][2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[t][g][e], sc, false));
-              w[t][2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[t][g][e], sc, true));
+              w[t][2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[vt][g][e], sc, false));
+              w[t][2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[vt][g][e], sc, true));
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < kE / 2; ++e) w[t][e] = v[t][g][e];
+            for (int e = 0; e < kE / 2; ++e) w[t][e] = v[vt][g][e];
           }
           if constexpr (CUT) {
 #pragma unroll
-            for (int e = 0; e < kE / 2; ++e) w[t][e] = (mask >> t) & 1u ? w[t][e] : 0u;
+            for (int e = 0; e < kE / 2; ++e) w[t][e] = (mask >> vt) & 1u ? w[t][e] : 0u;
           }
         }
 #pragma unroll
@@ -277,6 +280,7 @@ template <int KIND, int D> struct Wave {
           acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), pl, acc[g][e], 0, 0, 0);
         }
       }
+     }
     }
   }
 };
@@ -388,21 +392,22 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       int t0 = sp.base + sub0 * W::kSub;
       int page[W::kHalves];                            // of the tokens whose loads are issued next, requested one round ahead
       int64_t row[W::kHalves], scale[W::kHalves];
-      auto load_k = [&](bool there) {
+      const int until = min(len, sp.base + sub1 * W::kSub);   // nothing is fetched from here on
+      auto load_k = [&](int t) {
 #pragma unroll
         for (int h = 0; h < W::kHalves; ++h)
-          w.load_k(h, Rows(a.k + row[h], there ? 16 * W::kRow : 0), Rows(a.ks + scale[h], there ? 16 * W::kScaleRow : 0), n, c);
+          w.load_k(h, Rows(a.k + row[h], t + 16 * h < until ? 16 * W::kRow : 0), Rows(a.ks + scale[h], t + 16 * h < until ? 16 * W::kScaleRow : 0), n, c);
       };
-      auto load_v = [&](bool there) {
+      auto load_v = [&](int t) {
 #pragma unroll
         for (int h = 0; h < W::kHalves; ++h)
-          w.load_v(h, Rows(a.v + row[h], there ? 16 * W::kRow : 0), Rows(a.vs + scale[h], there ? 16 * W::kScaleRow : 0), n, c);
+          w.load_v(h, Rows(a.v + row[h], t + 16 * h < until ? 16 * W::kRow : 0), Rows(a.vs + scale[h], t + 16 * h < until ? 16 * W::kScaleRow : 0), n, c);
       };
 #pragma unroll
       for (int h = 0; h < W::kHalves; ++h) row_of(t0 + 16 * h, page_of(t0 + 16 * h), row[h], scale[h]);
-      load_k(true);
+      load_k(t0);
       __builtin_amdgcn_sched_barrier(0);               // the order of the rounds: keys are the older ones when scores wait for them
-      load_v(true);
+      load_v(t0);
 #pragma unroll
       for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + W::kStep + 16 * h);
       // The next keys are requested as soon as the scores are formed, the next values after the output, in the last round with a range of
@@ -412,11 +417,11 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
         w.scores(s, c);
 #pragma unroll
         for (int h = 0; h < W::kHalves; ++h) row_of(t0 + W::kStep + 16 * h, page[h], row[h], scale[h]);
-        load_k(i < rounds);
+        load_k(t0 + W::kStep);
 #pragma unroll
         for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kStep + 16 * h);
         const bool whole = t0 >= lo && t0 + W::kSub <= len;
-        uint32_t mask = 0xFFu;
+        uint32_t mask = ~0u;
         if (whole) {
 #pragma unroll
           for (int h = 0; h < W::kHalves; ++h) s[h] *= a.scale_log2;
@@ -434,8 +439,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
         }
         w.softmax(s);
         if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
-        load_v(i < rounds);
         t0 += W::kStep;
+        load_v(t0);
       }
     }
 
@@ -570,9 +575,9 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a) {
 
 // ---- host -------------------------------------------------------------------------------------------------
 struct Launch { int sub, tile_subs, parts, heads, blocks; int64_t most_subs; bool cut; };
-Launch launch_of(int dtype, int B, int Hq, int Hkv, int page_size, int max_pages, int window) {
+Launch launch_of(int dtype, int dim, int B, int Hq, int Hkv, int page_size, int max_pages, int window) {
   Launch l;
-  l.sub = dtype == MOE_F32 ? 16 : 32;
+  l.sub = 16 * attn_halves(dtype, dim);
   const int group = Hq / Hkv;
   l.parts = ceil_div(group, 16);
   l.heads = ceil_div(group, l.parts);
@@ -614,9 +619,12 @@ using namespace moe;
 
 extern "C" size_t moe_paged_attn_decode_workspace_bytes(int B, int Hq, int heads, int dim, int page_size, int max_pages) {
   if (B <= 0 || Hq <= 0 || heads <= 0 || dim <= 0 || page_size <= 0 || max_pages <= 0 || Hq % heads != 0) return 256;
-  const size_t f32 = ws_bytes_of(launch_of(MOE_F32, B, Hq, heads, page_size, max_pages, 0), B, heads, dim);
-  const size_t bf16 = ws_bytes_of(launch_of(MOE_BF16, B, Hq, heads, page_size, max_pages, 0), B, heads, dim);
-  return f32 > bf16 ? f32 : bf16;
+  size_t most = 256;
+  for (int dtype : {MOE_F32, MOE_BF16, MOE_MX8}) {
+    const size_t need = ws_bytes_of(launch_of(dtype, dim, B, Hq, heads, page_size, max_pages, 0), B, heads, dim);
+    if (need > most) most = need;
+  }
+  return most;
 }
 
 extern "C" int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int64_t q_stride_h, const moe_kv_cache_t* cache,
@@ -635,7 +643,7 @@ extern "C" int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int6
   MOE_REQUIRE(static_cast<int64_t>(cache->page_size) * max_pages < (int64_t{1} << 31) - 4096, MOE_ERR_UNSUPPORTED, "paged_attn_decode: contexts of %lld tokens",
               static_cast<long long>(cache->page_size) * max_pages);
   MOE_REQUIRE(static_cast<int64_t>(B) * Hq <= (1 << 23), MOE_ERR_UNSUPPORTED, "paged_attn_decode: B * Hq = %lld above 2^23", static_cast<long long>(B) * Hq);
-  const Launch l = launch_of(cache->dtype, B, Hq, cache->heads, cache->page_size, max_pages, window);
+  const Launch l = launch_of(cache->dtype, cache->dim, B, Hq, cache->heads, cache->page_size, max_pages, window);
   MOE_REQUIRE(l.most_subs < (int64_t{1} << 31) - 65536, MOE_ERR_UNSUPPORTED, "paged_attn_decode: %lld stretches of %d tokens", static_cast<long long>(l.most_subs), l.sub);
   const size_t need = moe_paged_attn_decode_workspace_bytes(B, Hq, cache->heads, cache->dim, cache->page_size, max_pages);
   MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "paged_attn_decode: workspace null, misaligned or smaller than %zu bytes", need);
