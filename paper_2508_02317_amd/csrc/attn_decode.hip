@@ -304,6 +304,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
   const int tile = a.tile_subs * W::kSub;
   auto span_of = [&](int len) { return attn_span(len, held, a.window, W::kSub, tile); };
   int len4[4], nt[4], mine = 0, incl = 0;              // of this lane's sequences: lengths, tiles of each, their sum, the sum up to and with this lane
+  bool empty = false;                                  // some sequence has no tokens
   auto count_from = [&](int b0) {
     mine = 0;
 #pragma unroll
@@ -315,6 +316,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
     for (int j = 0; j < 4; ++j) {
       nt[j] = span_of(len4[j]).tiles;
       mine += nt[j];
+      empty |= nt[j] == 0 && b0 + 4 * lane + j < a.B;
     }
     incl = wave_inclusive_sum(mine);
     return __builtin_amdgcn_readlane(incl, 63);
@@ -346,8 +348,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
     }
   }
 
-  // sequences without tokens
-  for (int b = me; b < a.B; b += static_cast<int>(gridDim.x)) {
+  for (int b = __any(empty) ? me : a.B; b < a.B; b += static_cast<int>(gridDim.x)) {
     if (span_of(lens[b]).tiles != 0) continue;
     for (int i = threadIdx.x; i < a.Hq * D; i += kThreads) static_cast<E*>(a.out)[static_cast<int64_t>(b) * a.Hq * D + i] = 0;
     if (a.lse)

@@ -140,6 +140,10 @@ def _load():
 
 
 lib = _load()
+try:
+    from . import _marshal              # csrc/marshal.cpp: the checks and the call of the functions that a generation step makes most
+except ImportError:                     # not built on this host: the same through ctypes
+    _marshal = None
 _raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
 
 
@@ -526,11 +530,14 @@ def moe_rope_table(freq, n_pos, amplitude=1.0, out=None):
     return cos, sin
 
 
-def _rope(call, q, k, positions, cos, sin, interleaved, out):
+def _rope(back, q, k, positions, cos, sin, interleaved, out):
+    if out is None:
+        out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    if _marshal is not None:
+        _check(_marshal.rope(back, q, k, positions, cos, sin, interleaved, out[0], out[1], _stream()))
+        return out
     some = q if q is not None else k
     dtype, (T, _, D) = some.dtype, some.shape
-    if out is None:
-        out = tuple(None if t is None else torch.empty(t.shape, dtype=dtype, device=some.device) for t in (q, k))
     qi = qo = ki = ko = _NO_HEADS
     Hq = Hk = 0
     if q is not None:
@@ -544,6 +551,7 @@ def _rope(call, q, k, positions, cos, sin, interleaved, out):
             raise ValueError("q and k must have the same tokens and head size")
         ki, ko = _heads(k, dtype, "k"), _heads(out[1], dtype, "k out", shape)
     p_pos, p_cos, p_sin, n_pos, rot = _table(cos, sin, positions, T)
+    call = lib.moe_rope_bwd if back else lib.moe_rope_fwd
     _check(call(*qi, *ki, _dtype_code(some), T, Hq, Hk, D, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, *ko, _stream()))
     return out
 
@@ -551,12 +559,12 @@ def _rope(call, q, k, positions, cos, sin, interleaved, out):
 def moe_rope_fwd(q, k, positions, cos, sin, interleaved=False, out=None):
     """q [T, Hq, D], k [T, Hk, D] (either may be None) rotated by positions [T] i32 with the table cos, sin [n_pos, rot / 2] f32.
     -> q_out, k_out; out = (q, k) rotates in place."""
-    return _rope(lib.moe_rope_fwd, q, k, positions, cos, sin, interleaved, out)
+    return _rope(False, q, k, positions, cos, sin, interleaved, out)
 
 
 def moe_rope_bwd(dq, dk, positions, cos, sin, interleaved=False, out=None):
     """Gradients of moe_rope_fwd's inputs from those of its outputs."""
-    return _rope(lib.moe_rope_bwd, dq, dk, positions, cos, sin, interleaved, out)
+    return _rope(True, dq, dk, positions, cos, sin, interleaved, out)
 
 
 class KVCacheView:
@@ -578,7 +586,7 @@ class KVCacheView:
         if code != MOE_MX8 and (k_scales is not None or v_scales is not None):
             raise ValueError("scales belong to a cache of 8-bit codes")
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
-        self.heads, self.dim, self.page_size = heads, dim, page_size
+        self.heads, self.dim, self.page_size, self.scale = heads, dim, page_size, dim ** -0.5
         self.desc = moe_kv_cache_t(code, pages, heads, page_size, dim, 0, _ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), k.stride(0),
                                    k_scales.stride(0) if code == MOE_MX8 else 0)
         self.ref = ctypes.addressof(self.desc)
@@ -593,6 +601,11 @@ def moe_kv_cache(k, v, k_scales=None, v_scales=None):
 def moe_kv_cache_write(cache, k, v, slots, q=None, positions=None, cos=None, sin=None, interleaved=False, q_out=None):
     """k, v [T, heads, dim] into the cache at slots [T] i64, the keys rotated if a table is given; q [T, Hq, dim] rotated into q_out.
     -> q_out (None without q)."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=cache.dtype, device=q.device)
+    if _marshal is not None:
+        _check(_marshal.kv_cache_write(cache.ref, k, v, slots, q, positions, cos, sin, interleaved, q_out, _stream()))
+        return q_out
     T, dt = k.shape[0], cache.dtype
     shape = (T, cache.heads, cache.dim)
     ki, vi = _heads(k, dt, "k", shape), _heads(v, dt, "v", shape)
@@ -603,8 +616,6 @@ def moe_kv_cache_write(cache, k, v, slots, q=None, positions=None, cos=None, sin
     Hq = 0
     if q is not None:
         Hq = q.shape[1]
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=q.device)
         qi, qo = _heads(q, dt, "q", (T, Hq, cache.dim)), _heads(q_out, dt, "q_out", q.shape)
     p_pos, p_cos, p_sin, n_pos, rot = _table(cos, sin, positions, T)
     _check(lib.moe_kv_cache_write(cache.ref, *ki, *vi, T, slots.data_ptr(), *qi, Hq, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, _stream()))
@@ -615,19 +626,22 @@ def moe_kv_cache_read(cache, pages, row_start, rows=None, first=None, out=None):
     """Tokens first[b] .. of every sequence b (first None: from its first on) into the rows row_start[b] .. row_start[b + 1] - 1.
     pages [B, max_pages] i32, row_start [B + 1] i32, first [B] i32; rows: row_start[B], needed without out.
     -> k, v [rows, heads, dim] in the cache's type (bf16 for 8-bit codes)."""
-    _need(pages, torch.int32, "pages"); _need(row_start, torch.int32, "row_start")
-    B, max_pages = pages.shape
-    if row_start.numel() != B + 1:
-        raise ValueError("row_start must be [%d]" % (B + 1))
-    if first is not None:
-        _need(first, torch.int32, "first")
-        if first.numel() != B:
-            raise ValueError("first must be [%d]" % B)
     if out is None:
         if rows is None:
             raise ValueError("rows (the last of row_start, on the host) or out must be given")
         out = tuple(torch.empty((rows, cache.heads, cache.dim), dtype=cache.dtype, device=pages.device) for _ in range(2))
     k, v = out
+    if _marshal is not None:
+        _check(_marshal.kv_cache_read(cache.ref, pages, row_start, first, k, v, _stream()))
+        return out
+    _need(pages, torch.int32, "pages"); _need(row_start, torch.int32, "row_start")
+    if pages.dim() != 2 or row_start.numel() != pages.shape[0] + 1:
+        raise ValueError("pages must be [sequences, max_pages] and row_start have one entry more than there are sequences")
+    B, max_pages = pages.shape
+    if first is not None:
+        _need(first, torch.int32, "first")
+        if first.numel() != B:
+            raise ValueError("first must be [%d]" % B)
     _need(k, cache.dtype, "k out"); _need(v, cache.dtype, "v out")
     if k.dim() != 3 or k.shape[1:] != (cache.heads, cache.dim) or v.shape != k.shape:
         raise ValueError("out must be two tensors [rows, %d, %d]" % (cache.heads, cache.dim))
@@ -639,22 +653,28 @@ def moe_kv_cache_read(cache, pages, row_start, rows=None, first=None, out=None):
 def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None, lse=None, ws=None):
     """Attention of one token per sequence: q [B, Hq, dim] over the first lens[b] tokens of the pages pages[b, :] (the last `window` of them
     where it is not 0).  scale None: dim ** -0.5.  -> out [B, Hq, dim], lse [B, Hq] f32 (None where lse is not given; True makes one)."""
+    if scale is None:
+        scale = cache.scale
+    if out is None:
+        out = torch.empty(q.shape, dtype=cache.dtype, device=q.device)
+    if lse is True:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if ws is None:
+        B, Hq, _ = q.shape
+        ws, _ = _ws(lib.moe_paged_attn_decode_workspace_bytes, (B, Hq, cache.heads, cache.dim, cache.page_size, pages.shape[1]), None, q.device)
+    if _marshal is not None:
+        _check(_marshal.paged_attn_decode(cache.ref, q, pages, lens, scale, window, out, lse, ws, _stream()))
+        return out, lse
     dt = cache.dtype
     B, Hq, _ = q.shape
     qi = _heads(q, dt, "q", (B, Hq, cache.dim))
     _need(pages, torch.int32, "pages"); _need(lens, torch.int32, "lens")
     if pages.dim() != 2 or pages.shape[0] != B or lens.numel() != B:
         raise ValueError("pages must be [%d, max_pages] and lens [%d]" % (B, B))
-    if out is None:
-        out = torch.empty((B, Hq, cache.dim), dtype=dt, device=q.device)
-    elif _need(out, dt, "out").shape != q.shape:
+    if _need(out, dt, "out").shape != q.shape:
         raise ValueError("out must have the shape of q")
-    if lse is True:
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
-    elif lse is not None and _need(lse, torch.float32, "lse").shape != (B, Hq):
+    if lse is not None and _need(lse, torch.float32, "lse").shape != (B, Hq):
         raise ValueError("lse must be [%d, %d]" % (B, Hq))
-    max_pages = pages.shape[1]
-    ws, nbytes = _ws(lib.moe_paged_attn_decode_workspace_bytes, (B, Hq, cache.heads, cache.dim, cache.page_size, max_pages), ws, q.device)
-    _check(lib.moe_paged_attn_decode(*qi, cache.ref, pages.data_ptr(), max_pages, lens.data_ptr(), B, Hq,
-                                     cache.dim ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse), ws.data_ptr(), nbytes, _stream()))
+    _check(lib.moe_paged_attn_decode(*qi, cache.ref, pages.data_ptr(), pages.shape[1], lens.data_ptr(), B, Hq, scale, window, out.data_ptr(), _ptr(lse),
+                                     ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
     return out, lse
