@@ -1,0 +1,56 @@
+"""Rotation frequencies and the book-keeping of pages (CPU only)."""
+import math
+
+import pytest
+import torch
+
+from paper_2508_02317_amd import generation as G
+
+
+def test_frequencies():
+    w = G.rope_frequencies(8, base=10000.0)
+    assert torch.allclose(w, torch.tensor([1.0, 0.1, 0.01, 0.001], dtype=torch.float64), rtol=1e-14)
+    assert torch.equal(G.rope_frequencies(8, scaling="linear", factor=4.0), w / 4)
+    b = G.rope_frequencies(8, scaling="base", factor=4.0)
+    assert b[0] == 1.0 and abs(b[-1] / w[-1] - 0.25) < 1e-14 and (b[1:-1] < w[1:-1]).all()
+    turns = 1000 * w / (2 * math.pi)                                  # 159, 15.9, 1.59, 0.159
+    p = G.rope_frequencies(8, scaling="parts", factor=4.0, original=1000, low=1.0, high=32.0)
+    assert p[0] == w[0] and torch.isclose(p[3], w[3] / 4, rtol=1e-14)
+    for i in (1, 2):
+        keep = (turns[i] - 1) / 31
+        assert torch.isclose(p[i], w[i] * (keep + (1 - keep) / 4), rtol=1e-14)
+    assert G.rope_amplitude(1.0) == 1.0 and abs(G.rope_amplitude(math.e) - 1.1) < 1e-15
+    for bad in (dict(rot=7), dict(rot=0), dict(rot=8, factor=0.5), dict(rot=2, scaling="base", factor=2.0), dict(rot=8, scaling="parts"), dict(rot=8, scaling="other"),
+                dict(rot=8, scaling="parts", original=100, low=2.0, high=2.0)):
+        with pytest.raises(ValueError):
+            G.rope_frequencies(**bad)
+
+
+@pytest.fixture
+def cache(monkeypatch):
+    monkeypatch.setattr(G.L, "moe_kv_cache", lambda k, v, ks, vs: None)          # no device here
+    return G.PagedKVCache(6, 16, 2, 64, device="cpu")
+
+
+def test_pages_are_handed_out_and_taken_back(cache):
+    cache.open("a"); cache.open("b")
+    slots, pos, table, lens = cache.grow(["a", "b"], [17, 16])
+    assert pos.tolist() == list(range(17)) + list(range(16)) and lens.tolist() == [17, 16]
+    assert slots.dtype is torch.int64 and table.dtype is torch.int32 and table.shape == (2, 2)
+    assert slots.tolist() == [int(table[0, t // 16]) * 16 + t % 16 for t in range(17)] + [int(table[1, 0]) * 16 + t for t in range(16)]
+    assert len(cache.free) == 3 and len(set(cache.pages_of["a"] + cache.pages_of["b"])) == 3
+    slots, pos, table, lens = cache.grow(["b"], [1])                            # into a page of its own
+    assert pos.tolist() == [16] and slots.tolist() == [int(table[0, 1]) * 16] and len(cache.free) == 2
+    before = dict(cache.length), {s: list(p) for s, p in cache.pages_of.items()}, list(cache.free)
+    with pytest.raises(MemoryError):
+        cache.grow(["a", "b"], [16, 32])                                        # three pages, two free
+    assert before == (cache.length, cache.pages_of, cache.free)
+    cache.grow(["a"], [0])
+    cache.close("a")
+    assert len(cache.free) == 4 and "a" not in cache.length
+    with pytest.raises(ValueError):
+        cache.open("b")
+    with pytest.raises(ValueError):
+        cache.grow(["b", "b"], [1, 1])
+    cache.close("b")
+    assert sorted(cache.free) == list(range(6))
