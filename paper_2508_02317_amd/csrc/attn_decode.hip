@@ -138,7 +138,7 @@ template <int KIND, int D> struct Wave {
   Words<kVWords> v[kVTokens][kNG];
   ScaleRow<kMx ? kScaleRow : 4> ks[kMx ? kHalves : 1];  // a token's scale bytes
   Words<kMx ? kScaleRow : 1> vs[kMx ? kHalves : 1];      // 4 tokens' scale bytes
-  u32x4 q[kQPieces];
+  u32x4 q[kQPieces], q_next[kQPieces];                   // of this part of the piece and of the next
   f32x4 acc[kNG][kE];
   float m, l;
 
@@ -147,8 +147,12 @@ template <int KIND, int D> struct Wave {
     for (int i = 0; i < kQPieces; ++i) {
       // the elements that the keys' lane holds: bytes 64 i + 16 c on, or for 8-bit keys the elements 64 (i / 2) + 16 c + 8 (i % 2) on
       const int at = kMx ? ((i / 2) * 64 + c * 16 + (i % 2) * 8) * 2 : i * 64 + c * 16;
-      q[i] = *reinterpret_cast<const u32x4*>(head_row + at);
+      q_next[i] = *reinterpret_cast<const u32x4*>(head_row + at);
     }
+  }
+  __device__ __forceinline__ void take_q() {
+#pragma unroll
+    for (int i = 0; i < kQPieces; ++i) q[i] = q_next[i];
   }
   __device__ __forceinline__ void begin() {
     m = -INFINITY;
@@ -324,7 +328,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
   int total = 0;
   for (int b0 = 0; b0 < a.B; b0 += 256) total += count_from(b0);
   const AttnCut cut = attn_cut(total * units, static_cast<int>(gridDim.x));
-  int at = attn_begin(cut, me);
+  const int at = attn_begin(cut, me);
   const int end = attn_begin(cut, me + 1);
   int b_at = 0, before = 0, len_at = 0;                // sequence of tile `at`, tiles (of one unit) of the sequences before it, its length
   if (at < end) {
@@ -357,92 +361,128 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       for (int i = threadIdx.x; i < units; i += kThreads) a.unit_pieces[2 * (static_cast<int64_t>(b) * units + i)] = -1;
   }
 
-  while (at < end) {
+  // A stretch of the piece within one unit (a sequence and a group of heads), and what of it is this wave's: every fourth of its stretches of
+  // kSub tokens, `rounds` of them from token t0 on; nothing is fetched from `until` on.
+  struct Part {
+    int b, head0, heads, kv, unit_begin, unit_end, first, last, lo, len, t0, rounds, until, u;
+    ScalarInts pages;
+  };
+  auto part_at = [&](int tile) {
     AttnSpan sp = span_of(len_at);
-    while (at >= (before + sp.tiles) * units) {        // on to the sequence that has the tile
+    while (tile >= (before + sp.tiles) * units) {      // on to the sequence that has the tile
       before += sp.tiles;
       len_at = lens[++b_at];
       sp = span_of(len_at);
     }
-    const int u = (at - before * units) / sp.tiles, unit_begin = before * units + u * sp.tiles, unit_end = unit_begin + sp.tiles;
-    const int first = at, last = min(end, unit_end);
-    const int kv = u / a.parts, part = u - kv * a.parts, head0 = kv * a.group + part * a.heads, heads = min(a.heads, a.group - part * a.heads);
-    const int lo = sp.lo, len = sp.len;
-
-    W w;
-    {
-      const int h = head0 + min(n, heads - 1);         // columns without a head repeat the last one's
-      w.load_q(static_cast<const char*>(a.q) + (static_cast<int64_t>(b_at) * a.q_stride_b + static_cast<int64_t>(h) * a.q_stride_h) * static_cast<int>(sizeof(E)), c);
+    Part q;
+    q.b = b_at;
+    q.u = (tile - before * units) / sp.tiles;
+    q.unit_begin = before * units + q.u * sp.tiles;
+    q.unit_end = q.unit_begin + sp.tiles;
+    q.first = tile;
+    q.last = min(end, q.unit_end);
+    q.kv = q.u / a.parts;
+    const int part = q.u - q.kv * a.parts;
+    q.head0 = q.kv * a.group + part * a.heads;
+    q.heads = min(a.heads, a.group - part * a.heads);
+    q.lo = sp.lo;
+    q.len = sp.len;
+    const int sub0 = (tile - q.unit_begin) * a.tile_subs + wave, sub1 = min((q.last - q.unit_begin) * a.tile_subs, (sp.len - sp.base + W::kSub - 1) / W::kSub);
+    q.t0 = sp.base + sub0 * W::kSub;
+    q.rounds = sub0 < sub1 ? (sub1 - sub0 + kWaves - 1) / kWaves : 0;
+    q.until = sub0 < sub1 ? min(sp.len, sp.base + sub1 * W::kSub) : 0;
+    q.pages = scalar_ints(a.block_table + static_cast<int64_t>(b_at) * a.max_pages);
+    return q;
+  };
+  const int page_mask = (1 << a.page_shift) - 1;
+  // A half of 16 tokens that begins at token t lies in one page.  A half without tokens takes the nearest one that has some, and is masked.
+  auto near = [&](const Part& q, int t) { return min(max(t, q.lo), q.len - 1); };
+  W w;
+  int page[W::kHalves];                                // of the tokens whose loads are issued next, requested one round ahead
+  int64_t row[W::kHalves], scale[W::kHalves];
+  auto find_pages = [&](const Part& q, int t) {
+#pragma unroll
+    for (int h = 0; h < W::kHalves; ++h) page[h] = q.pages[near(q, t + 16 * h) >> a.page_shift];
+  };
+  auto load_k = [&](const Part& q, int t) {            // into the pages that were found, whose rows the values' loads use too
+#pragma unroll
+    for (int h = 0; h < W::kHalves; ++h) {
+      const int in_page = (q.kv << a.page_shift) + (near(q, t + 16 * h) & page_mask & ~15);
+      const int64_t p = min(max(page[h], 0), a.pages - 1);
+      row[h] = p * a.page_bytes + static_cast<int64_t>(in_page) * W::kRow;
+      scale[h] = p * a.scale_page_bytes + static_cast<int64_t>(in_page) * W::kScaleRow;
     }
+#pragma unroll
+    for (int h = 0; h < W::kHalves; ++h) {
+      const bool there = t + 16 * h < q.until;
+      w.load_k(h, Rows(a.k + row[h], there ? 16 * W::kRow : 0), Rows(a.ks + scale[h], there ? 16 * W::kScaleRow : 0), n, c);
+    }
+  };
+  auto load_v = [&](const Part& q, int t) {
+#pragma unroll
+    for (int h = 0; h < W::kHalves; ++h) {
+      const bool there = t + 16 * h < q.until;
+      w.load_v(h, Rows(a.v + row[h], there ? 16 * W::kRow : 0), Rows(a.vs + scale[h], there ? 16 * W::kScaleRow : 0), n, c);
+    }
+  };
+  auto load_q = [&](const Part& q) {
+    const int h = q.head0 + min(n, q.heads - 1);       // columns without a head repeat the last one's
+    w.load_q(static_cast<const char*>(a.q) + (static_cast<int64_t>(q.b) * a.q_stride_b + static_cast<int64_t>(h) * a.q_stride_h) * static_cast<int>(sizeof(E)), c);
+  };
+  if (at >= end) return;
+  Part cur = part_at(at);
+  load_q(cur);
+  find_pages(cur, cur.t0);
+  load_k(cur, cur.t0);
+  __builtin_amdgcn_sched_barrier(0);                   // the order of the rounds: keys are the older ones when scores wait for them
+  load_v(cur, cur.t0);
+
+  for (;;) {
+    // what comes after this part; behind the piece's end: this part again, with nothing to fetch
+    Part next = cur;
+    next.until = next.rounds = 0;
+    if (cur.last < end) next = part_at(cur.last);
+    const int lo = cur.lo, len = cur.len, heads = cur.heads;
+    w.take_q();
+    load_q(next);
     w.begin();
-    const ScalarInts pages = scalar_ints(a.block_table + static_cast<int64_t>(b_at) * a.max_pages);
-    const int page_mask = (1 << a.page_shift) - 1;
-    // A half of 16 tokens that begins at token t lies in one page.  A half without tokens takes the nearest one that has some, and is masked.
-    auto near = [&](int t) { return min(max(t, lo), len - 1); };
-    auto page_of = [&](int t) { return pages[near(t) >> a.page_shift]; };
-    auto row_of = [&](int t, int page, int64_t& rows, int64_t& scales) {
-      const int row = (kv << a.page_shift) + (near(t) & page_mask & ~15);
-      const int64_t p = min(max(page, 0), a.pages - 1);
-      rows = p * a.page_bytes + static_cast<int64_t>(row) * W::kRow;
-      scales = p * a.scale_page_bytes + static_cast<int64_t>(row) * W::kScaleRow;
-    };
-    // the wave takes every fourth of the piece's stretches of kSub tokens
-    const int sub0 = (first - unit_begin) * a.tile_subs + wave, sub1 = min((last - unit_begin) * a.tile_subs, (len - sp.base + W::kSub - 1) / W::kSub);
-    const int rounds = (sub1 - sub0 + kWaves - 1) / kWaves;
-    if (sub0 < sub1) {
-      int t0 = sp.base + sub0 * W::kSub;
-      int page[W::kHalves];                            // of the tokens whose loads are issued next, requested one round ahead
-      int64_t row[W::kHalves], scale[W::kHalves];
-      const int until = min(len, sp.base + sub1 * W::kSub);   // nothing is fetched from here on
-      auto load_k = [&](int t) {
+    int t0 = cur.t0;
+    if (cur.rounds > 1) find_pages(cur, t0 + W::kStep); else find_pages(next, next.t0);
+    // The next keys are requested as soon as the scores are formed, the next values after the output, the first ones of the next part among
+    // them, and where nothing follows with a range of nothing: without branches around the requests a wait for older ones leaves the younger
+    // ones in flight.
+    for (int i = 1; i <= cur.rounds; ++i) {
+      f32x4 s[W::kHalves];
+      w.scores(s, c);
+      const Part& from = i < cur.rounds ? cur : next;
+      const int t1 = i < cur.rounds ? t0 + W::kStep : next.t0;
+      load_k(from, t1);
+      if (i + 1 < cur.rounds) find_pages(cur, t1 + W::kStep); else find_pages(next, next.t0);
+      const bool whole = t0 >= lo && t0 + W::kSub <= len;
+      uint32_t mask = ~0u;
+      if (whole) {
+#pragma unroll
+        for (int h = 0; h < W::kHalves; ++h) s[h] *= a.scale_log2;
+      } else {
+        mask = 0u;
 #pragma unroll
         for (int h = 0; h < W::kHalves; ++h)
-          w.load_k(h, Rows(a.k + row[h], t + 16 * h < until ? 16 * W::kRow : 0), Rows(a.ks + scale[h], t + 16 * h < until ? 16 * W::kScaleRow : 0), n, c);
-      };
-      auto load_v = [&](int t) {
 #pragma unroll
-        for (int h = 0; h < W::kHalves; ++h)
-          w.load_v(h, Rows(a.v + row[h], t + 16 * h < until ? 16 * W::kRow : 0), Rows(a.vs + scale[h], t + 16 * h < until ? 16 * W::kScaleRow : 0), n, c);
-      };
-#pragma unroll
-      for (int h = 0; h < W::kHalves; ++h) row_of(t0 + 16 * h, page_of(t0 + 16 * h), row[h], scale[h]);
-      load_k(t0);
-      __builtin_amdgcn_sched_barrier(0);               // the order of the rounds: keys are the older ones when scores wait for them
-      load_v(t0);
-#pragma unroll
-      for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + W::kStep + 16 * h);
-      // The next keys are requested as soon as the scores are formed, the next values after the output, in the last round with a range of
-      // nothing: without branches around the requests a wait for older ones leaves the younger ones in flight.
-      for (int i = 1; i <= rounds; ++i) {
-        f32x4 s[W::kHalves];
-        w.scores(s, c);
-#pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) row_of(t0 + W::kStep + 16 * h, page[h], row[h], scale[h]);
-        load_k(t0 + W::kStep);
-#pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) page[h] = page_of(t0 + 2 * W::kStep + 16 * h);
-        const bool whole = t0 >= lo && t0 + W::kSub <= len;
-        uint32_t mask = ~0u;
-        if (whole) {
-#pragma unroll
-          for (int h = 0; h < W::kHalves; ++h) s[h] *= a.scale_log2;
-        } else {
-          mask = 0u;
-#pragma unroll
-          for (int h = 0; h < W::kHalves; ++h)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int t = t0 + 16 * h + 4 * c + r;
-              const bool there = t >= lo && t < len;
-              mask |= there ? 1u << (4 * h + r) : 0u;
-              s[h][r] = there ? s[h][r] * a.scale_log2 : -INFINITY;
-            }
-        }
-        w.softmax(s);
-        if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
-        t0 += W::kStep;
-        load_v(t0);
+          for (int r = 0; r < 4; ++r) {
+            const int t = t0 + 16 * h + 4 * c + r;
+            const bool there = t >= lo && t < len;
+            mask |= there ? 1u << (4 * h + r) : 0u;
+            s[h][r] = there ? s[h][r] * a.scale_log2 : -INFINITY;
+          }
       }
+      w.softmax(s);
+      if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
+      load_v(from, t1);
+      t0 = t1;
+    }
+    if (cur.rounds == 0) {                             // nothing of this part was this wave's, so nothing has been requested behind it
+      load_k(next, next.t0);
+      load_v(next, next.t0);
     }
 
     // the four waves' parts, and out
@@ -466,8 +506,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       }
     }
     __syncthreads();
-    const bool complete = first == unit_begin && last == unit_end;
-    const int slot = 2 * me + (first == attn_begin(cut, me) ? 0 : 1);
+    const bool complete = cur.first == cur.unit_begin && cur.last == cur.unit_end;
+    const int slot = 2 * me + (cur.first == at ? 0 : 1);
     for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
       const int h = i / (D / 4), d = (i - h * (D / 4)) * 4;
       const float m = fmaxf(fmaxf(s_m[0][h], s_m[1][h]), fmaxf(s_m[2][h], s_m[3][h]));
@@ -479,7 +519,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
         o += *reinterpret_cast<const f32x4*>(&s_out[v][h][d]);
       }
       if (complete) {
-        const int64_t row = static_cast<int64_t>(b_at) * a.Hq + head0 + h;
+        const int64_t row = static_cast<int64_t>(cur.b) * a.Hq + cur.head0 + h;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         if constexpr (KIND == MOE_F32) {
           *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + row * D + d) = o * inv;
@@ -493,12 +533,13 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
         if (d == 0) { to[0] = m; to[1] = sum; }
       }
     }
-    if (a.unit_pieces && threadIdx.x == 0 && first == unit_begin) {
-      int32_t* p = a.unit_pieces + 2 * (static_cast<int64_t>(b_at) * units + u);
+    if (a.unit_pieces && threadIdx.x == 0 && cur.first == cur.unit_begin) {
+      int32_t* p = a.unit_pieces + 2 * (static_cast<int64_t>(cur.b) * units + cur.u);
       p[0] = complete ? -1 : slot;
-      p[1] = attn_owner(cut, unit_end - 1);
+      p[1] = attn_owner(cut, cur.unit_end - 1);
     }
-    at = last;
+    if (cur.last >= end) return;
+    cur = next;
   }
 }
 
