@@ -44,7 +44,8 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x1 __attribute__((ext_vector_type(1)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr double kLog2e = 1.44269504088896340736;
+constexpr float kLn2 = 0.69314718055994530942f;
 
 struct Args {
   const void* q;
@@ -54,7 +55,7 @@ struct Args {
   int pages, page_shift;
   const int32_t *block_table, *lens;
   int max_pages, B, Hq, Hkv, group, parts, heads;      // group: query heads per key head, in `parts` units of up to `heads`
-  float scale_log2;
+  float scale_hi, scale_lo;                            // together scale log2 e
   int window, tile_subs;                              // tile_subs: stretches of kSub tokens in a tile, four of them or a whole context
   void* out;
   float* lse;
@@ -181,34 +182,51 @@ template <int KIND, int D> struct Wave {
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
     return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
   }
+  // In fp32, four products of one chain of additions after the other: two chains are half as long, in time and in rounding.
+  static constexpr int kChains = kF32 ? 2 : 1;
   __device__ __forceinline__ void scores(f32x4 (&s)[kHalves], int c) const {
+    f32x4 t[kHalves][kChains];
 #pragma unroll
-    for (int a = 0; a < kHalves; ++a) s[a] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int a = 0; a < kHalves; ++a)
+#pragma unroll
+      for (int u = 0; u < kChains; ++u) t[a][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kKPieces; ++i)
 #pragma unroll
       for (int a = 0; a < kHalves; ++a) {
         if constexpr (kF32) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[i][j]), s[a], 0, 0, 0);
+          for (int j = 0; j < 4; ++j)
+            t[a][j % kChains] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[i][j]), t[a][j % kChains], 0, 0, 0);
         } else if constexpr (kMx) {
           const float sc = scale_of((ks[a].pair(i) >> (8 * (c >> 1))) & 0xFFu);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, q[2 * i + h]), s[a], 0, 0, 0);
-          }
+          for (int h = 0; h < 2; ++h)
+            t[a][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, q[2 * i + h]), t[a][0], 0, 0, 0);
         } else {
-          s[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[a][i]), __builtin_bit_cast(bf16x8, q[i]), s[a], 0, 0, 0);
+          t[a][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[a][i]), __builtin_bit_cast(bf16x8, q[i]), t[a][0], 0, 0, 0);
         }
       }
+#pragma unroll
+    for (int a = 0; a < kHalves; ++a) {
+      s[a] = t[a][0];
+#pragma unroll
+      for (int u = 1; u < kChains; ++u) s[a] += t[a][u];
+    }
   }
-  // p of the scores, with the running maximum, sum and output brought to the new maximum
-  __device__ __forceinline__ void softmax(f32x4 (&s)[kHalves]) {
+  // p of the scores, with the running maximum, sum and output brought to the new maximum.  Exponents are of 2: x = s (hi + lo) with
+  // hi + lo = scale log2 e.  The maximum is one of the rounded products s hi; an exponent is formed from s anew, so that it has
+  // the rounding of a small difference and not that of the product.  `mask`: bit 4 a + r set where this lane's token exists.
+  __device__ __forceinline__ void softmax(f32x4 (&s)[kHalves], float hi, float lo, uint32_t mask) {
+    f32x4 x[kHalves];
     float top = -INFINITY;
 #pragma unroll
     for (int a = 0; a < kHalves; ++a)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[a][r]);
+      for (int r = 0; r < 4; ++r) {
+        x[a][r] = (mask >> (4 * a + r)) & 1u ? s[a][r] * hi : -INFINITY;
+        top = fmaxf(top, x[a][r]);
+      }
     top = fmaxf(m, row_max4(top));
     if (__any(top > m)) {
       const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;   // m = -inf: 0
@@ -219,12 +237,13 @@ template <int KIND, int D> struct Wave {
         for (int e = 0; e < kE; ++e) acc[g][e] *= f;
       m = top;
     }
-    const float base = m > -INFINITY ? m : 0.0f;       // all scores so far -inf: p = exp2(-inf) = 0
+    const float base = m > -INFINITY ? m : 0.0f;
 #pragma unroll
     for (int a = 0; a < kHalves; ++a)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        s[a][r] = __builtin_amdgcn_exp2f(s[a][r] - base);
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[a][r], lo, fmaf(s[a][r], hi, -base)));
+        s[a][r] = x[a][r] == -INFINITY ? 0.0f : p;     // masked, or a score of -inf: no weight (and a NaN stays one)
         l += s[a][r];
       }
   }
@@ -460,22 +479,17 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       if (i + 1 < cur.rounds) find_pages(cur, t1 + W::kStep); else find_pages(next, next.t0);
       const bool whole = t0 >= lo && t0 + W::kSub <= len;
       uint32_t mask = ~0u;
-      if (whole) {
-#pragma unroll
-        for (int h = 0; h < W::kHalves; ++h) s[h] *= a.scale_log2;
-      } else {
+      if (!whole) {
         mask = 0u;
 #pragma unroll
         for (int h = 0; h < W::kHalves; ++h)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int t = t0 + 16 * h + 4 * c + r;
-            const bool there = t >= lo && t < len;
-            mask |= there ? 1u << (4 * h + r) : 0u;
-            s[h][r] = there ? s[h][r] * a.scale_log2 : -INFINITY;
+            mask |= t >= lo && t < len ? 1u << (4 * h + r) : 0u;
           }
       }
-      w.softmax(s);
+      w.softmax(s, a.scale_hi, a.scale_lo, mask);
       if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
       load_v(from, t1);
       t0 = t1;
@@ -697,7 +711,7 @@ extern "C" int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int6
   a.scale_page_bytes = cache->scale_page_stride;
   a.pages = cache->pages; a.page_shift = __builtin_ctz(cache->page_size);
   a.block_table = block_table; a.lens = lens; a.max_pages = max_pages; a.B = B; a.Hq = Hq; a.Hkv = cache->heads; a.group = Hq / cache->heads;
-  a.parts = l.parts; a.heads = l.heads; a.scale_log2 = scale * kLog2e; a.window = window; a.tile_subs = l.tile_subs; a.out = out; a.lse = lse;
+  a.parts = l.parts; a.heads = l.heads; a.scale_hi = static_cast<float>(scale * kLog2e); a.scale_lo = static_cast<float>(scale * kLog2e - a.scale_hi); a.window = window; a.tile_subs = l.tile_subs; a.out = out; a.lse = lse;
   if (l.cut) {
     a.unit_pieces = static_cast<int32_t*>(ws);
     a.slots = reinterpret_cast<float*>(static_cast<char*>(ws) + pieces_bytes(B, cache->heads, l.parts));
