@@ -6,8 +6,8 @@
 // with the pair (i, i + rot/2), or (2i, 2i + 1) where neighbours are paired; elements from rot on stay as they are.  The turn is a
 // rotation, so its gradient is the turn by the opposite angle.
 //
-// Everything here moves bytes and is bound by HBM.  A lane owns 8 consecutive elements of a head, so that every access to a tensor is 16
-// bytes or more per lane and a head row is contiguous over its lanes; a row's lanes lie in one wave (8 to 64 of them, rounded up to a power of two).
+// Everything here moves bytes and is bound by HBM.  A lane owns 16 consecutive bytes of a head, so that a head row
+// is contiguous over its lanes in every access; a row's lanes lie in one wave (up to 64 of them, rounded up to a power of two).
 // The partner elements of the half layout come from the lane that owns them, not from memory again: a row is read whole before any
 // of it is written, which makes the turn in place safe, and is read once.  The cosines and sines of a token are read once per lane and used for
 // all heads that the lane walks.
@@ -33,9 +33,9 @@ constexpr int kMaxBlocksX = 1 << 20;                   // a workgroup walks on w
 
 __device__ __forceinline__ int wave_of_block() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6); }
 
-// Eight consecutive elements as they lie in memory.
-template <class E> struct Eight;
-template <> struct Eight<bf16_t> {
+// N consecutive elements of a head row as they lie in memory: 16 bytes, or 32 in fp32 rows of more than 64 pieces of 16.
+template <class E, int N> struct Piece;
+template <> struct Piece<bf16_t, 8> {
   u32x4 w;
   __device__ __forceinline__ void load(const bf16_t* p) { w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
   __device__ __forceinline__ void store(bf16_t* p) const { __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p)); }
@@ -47,78 +47,92 @@ template <> struct Eight<bf16_t> {
 #pragma unroll
     for (int q = 0; q < 4; ++q) w[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
   }
-  __device__ __forceinline__ Eight of_lane(int lane) const {
-    Eight o;
+  __device__ __forceinline__ Piece of_lane(int lane) const {
+    Piece o;
 #pragma unroll
     for (int q = 0; q < 4; ++q) o.w[q] = __shfl(w[q], lane, 64);
     return o;
   }
 };
-template <> struct Eight<float> {
-  f32x4 a, b;
+template <int N> struct Piece<float, N> {
+  f32x4 w[N / 4];
   __device__ __forceinline__ void load(const float* p) {
-    a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
-    b = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1);
+#pragma unroll
+    for (int g = 0; g < N / 4; ++g) w[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + g);
   }
   __device__ __forceinline__ void store(float* p) const {
-    __builtin_nontemporal_store(a, reinterpret_cast<f32x4*>(p));
-    __builtin_nontemporal_store(b, reinterpret_cast<f32x4*>(p) + 1);
-  }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) { v[q] = a[q]; v[4 + q] = b[q]; }
+    for (int g = 0; g < N / 4; ++g) __builtin_nontemporal_store(w[g], reinterpret_cast<f32x4*>(p) + g);
   }
-  __device__ __forceinline__ void set(const float (&v)[8]) {
+  __device__ __forceinline__ void get(float (&v)[N]) const {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) { a[q] = v[q]; b[q] = v[4 + q]; }
+    for (int q = 0; q < N; ++q) v[q] = w[q / 4][q % 4];
   }
-  __device__ __forceinline__ Eight of_lane(int lane) const {
-    Eight o;
+  __device__ __forceinline__ void set(const float (&v)[N]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) { o.a[q] = __shfl(a[q], lane, 64); o.b[q] = __shfl(b[q], lane, 64); }
+    for (int q = 0; q < N; ++q) w[q / 4][q % 4] = v[q];
+  }
+  __device__ __forceinline__ Piece of_lane(int lane) const {
+    Piece o;
+#pragma unroll
+    for (int q = 0; q < N; ++q) o.w[q / 4][q % 4] = __shfl(w[q / 4][q % 4], lane, 64);
     return o;
   }
 };
+// N table values, or one for every two
+template <int N> __device__ __forceinline__ void load_table(float (&v)[N], const float* p) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int g = 0; g < N / 4; ++g) {
+      const f32x4 x = reinterpret_cast<const f32x4*>(p)[g];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[4 * g + q] = x[q];
+    }
+  } else {
+    const f32x2 x = *reinterpret_cast<const f32x2*>(p);
+    v[0] = x[0];
+    v[1] = x[1];
+  }
+}
 
 // ---- the turn, with or without a cache behind it ----------------------------------------------------------
 // A wave has one token at a time and walks its head rows, 64 / lanes of them next to each other in memory per access and kAtOnce
 // accesses in flight.  (A wave over as many tokens instead, a head
 // row of each, moves 256-byte pieces: 40960 tokens of 32 + 4 heads 142 us, as it is 124.)
-template <class E, int CACHE /* 0: none, 1: elements as they are, 2: 8-bit blocks */>
+template <class E, int N, int CACHE /* 0: none, 1: elements as they are, 2: 8-bit blocks */>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lanes, int heads_per_block) {
   const int lane = static_cast<int>(threadIdx.x) & 63, chunk = lane & (lanes - 1), sub = lane / lanes, abreast = 64 / lanes;
-  if (chunk * 8 >= a.D) return;                        // lanes of the power of two that a head row has no elements for
+  if (chunk * N >= a.D) return;                        // lanes of the power of two that a head row has no elements for
   const int half = a.rot / 2;
-  const bool turned = chunk * 8 < a.rot, first = chunk * 8 < half;
-  const int partner = !turned ? lane : first ? lane + half / 8 : lane - half / 8;
+  const bool turned = chunk * N < a.rot, first = chunk * N < half;
+  const int partner = !turned ? lane : first ? lane + half / N : lane - half / N;
   const int turned_rows = a.Hq + a.Hk, rows = turned_rows + a.Hv;
   const int h0 = blockIdx.y * heads_per_block, h1 = min(rows, h0 + heads_per_block);
 
   for (long t = static_cast<long>(blockIdx.x) * kWaves + wave_of_block(); t < a.T; t += static_cast<long>(gridDim.x) * kWaves) {
-    float co[8], si[8];
+    float co[N], si[N];
     if (turned && h0 < turned_rows) {
       const int p = min(max(a.positions[t], 0), a.n_pos - 1);
       if (a.interleaved) {
-        const long at = static_cast<long>(p) * half + chunk * 4;
-        const f32x4 c = *reinterpret_cast<const f32x4*>(a.cos + at), s = *reinterpret_cast<const f32x4*>(a.sin + at);
+        const long at = static_cast<long>(p) * half + chunk * (N / 2);
+        float c[N / 2], s[N / 2];
+        load_table(c, a.cos + at);
+        load_table(s, a.sin + at);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          co[2 * q] = co[2 * q + 1] = c[q];
-          si[2 * q] = a.back ? s[q] : -s[q];
-          si[2 * q + 1] = -si[2 * q];
+        for (int q = 0; q < N; ++q) {
+          co[q] = c[q / 2];
+          si[q] = (q % 2 == 0) == (a.back != 0) ? s[q / 2] : -s[q / 2];
         }
       } else {
-        const long at = static_cast<long>(p) * half + (first ? chunk * 8 : chunk * 8 - half);
+        const long at = static_cast<long>(p) * half + (first ? chunk * N : chunk * N - half);
+        load_table(co, a.cos + at);
+        load_table(si, a.sin + at);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const f32x4 c = reinterpret_cast<const f32x4*>(a.cos + at)[g], s = reinterpret_cast<const f32x4*>(a.sin + at)[g];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) { co[4 * g + q] = c[q]; si[4 * g + q] = first == (a.back != 0) ? s[q] : -s[q]; }
-        }
+        for (int q = 0; q < N; ++q) si[q] = first == (a.back != 0) ? si[q] : -si[q];
       }
     } else {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) { co[q] = 1.0f; si[q] = 0.0f; }
+      for (int q = 0; q < N; ++q) { co[q] = 1.0f; si[q] = 0.0f; }
     }
     long slot = -1;
     if (CACHE != 0 && h1 > a.Hq) {
@@ -129,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lane
     const long page = slot >> page_shift, place = slot & (a.cache.page_size - 1);
 
     for (int h = h0 + sub; h < h1; h += abreast * kAtOnce) {
-      Eight<E> x[kAtOnce];
+      Piece<E, N> x[kAtOnce];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         const int i = h + u * abreast;
@@ -137,44 +151,44 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lane
         const bool is_q = i < a.Hq, is_v = i >= turned_rows;
         const E* src = static_cast<const E*>(is_q ? a.q : is_v ? a.v : a.k);
         const long st = is_q ? a.q_stride_t : is_v ? a.v_stride_t : a.k_stride_t, sh = is_q ? a.q_stride_h : is_v ? a.v_stride_h : a.k_stride_h;
-        x[u].load(src + t * st + (is_q ? i : is_v ? i - turned_rows : i - a.Hq) * sh + chunk * 8);
+        x[u].load(src + t * st + (is_q ? i : is_v ? i - turned_rows : i - a.Hq) * sh + chunk * N);
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         const int i = h + u * abreast;
         if (i >= h1) break;
         const bool is_q = i < a.Hq, is_v = i >= turned_rows;
-        float y[8];
+        float y[N];
         x[u].get(y);
         if (!is_v) {
-          float other[8];
+          float other[N];
           if (a.interleaved) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) other[q] = y[q ^ 1];
+            for (int q = 0; q < N; ++q) other[q] = y[q ^ 1];
           } else {
             x[u].of_lane(partner).get(other);
           }
           if (turned) {
 #pragma clang fp contract(off)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
+            for (int q = 0; q < N; ++q) {
               const float own = y[q] * co[q], turn = other[q] * si[q];
               y[q] = own + turn;
             }
           }
         }
-        Eight<E> o = x[u];
+        Piece<E, N> o = x[u];
         if (!is_v && turned) o.set(y);
         if (CACHE == 0 || is_q) {
           E* dst = static_cast<E*>(is_q ? a.q_out : a.k_out);
           const long st = is_q ? a.qo_stride_t : a.ko_stride_t, sh = is_q ? a.qo_stride_h : a.ko_stride_h;
-          o.store(dst + t * st + (is_q ? i : i - a.Hq) * sh + chunk * 8);
+          o.store(dst + t * st + (is_q ? i : i - a.Hq) * sh + chunk * N);
         } else {
           const long row = static_cast<long>(is_v ? i - turned_rows : i - a.Hq) * a.cache.page_size + place;
           void* base = is_v ? a.cache.v : a.cache.k;
           if (CACHE == 1) {
-            if (slot >= 0) o.store(static_cast<E*>(base) + page * a.cache.page_stride + row * a.D + chunk * 8);
-          } else {
+            if (slot >= 0) o.store(static_cast<E*>(base) + page * a.cache.page_stride + row * a.D + chunk * N);
+          } else if constexpr (CACHE == 2) {
             float amax = 0.0f;
 #pragma unroll
             for (int q = 0; q < 8; ++q) amax = fmaxf(amax, fabsf(y[q]));
@@ -194,19 +208,19 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lane
   }
 }
 
-int lanes_of_row(int D) {
+int lanes_of_row(int D, int n) {
   int lanes = 1;
-  while (lanes * 8 < D) lanes *= 2;
+  while (lanes * n < D) lanes *= 2;
   return lanes;
 }
 
-template <class E, int CACHE> void launch_rotate(const char* name, const RotateArgs& a) {
-  const int lanes = lanes_of_row(a.D), step = 64 / lanes * kAtOnce, rows = a.Hq + a.Hk + a.Hv;
+template <class E, int N, int CACHE> void launch_rotate(const char* name, const RotateArgs& a) {
+  const int lanes = lanes_of_row(a.D, N), step = 64 / lanes * kAtOnce, rows = a.Hq + a.Hk + a.Hv;
   const int bx = static_cast<int>(a.T / kWaves + (a.T % kWaves != 0)), gx = bx < kMaxBlocksX ? bx : kMaxBlocksX;
   // heads are cut into as many blocks as it takes to have kBlocksWanted workgroups; a block is a multiple of what a wave has in flight
   const int want = ceil_div(kBlocksWanted, gx), most = ceil_div(rows, step), cut = want < most ? want : most;
   const int heads = ceil_div(ceil_div(rows, cut), step) * step;
-  MOE_LAUNCH(name, (rotate_kernel<E, CACHE>), dim3(gx, ceil_div(rows, heads)), dim3(kThreads), 0, a.stream, a, lanes, heads);
+  MOE_LAUNCH(name, (rotate_kernel<E, N, CACHE>), dim3(gx, ceil_div(rows, heads)), dim3(kThreads), 0, a.stream, a, lanes, heads);
 }
 
 // ---- back from the pages ----------------------------------------------------------------------------------
@@ -217,6 +231,7 @@ template <class E, int CACHE> void launch_rotate(const char* name, const RotateA
 template <int KIND /* MOE_F32, MOE_BF16 or MOE_MX8 */>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, int lanes, int heads_per_block) {
   typedef std::conditional_t<KIND == MOE_F32, float, bf16_t> E;
+  constexpr int N = 16 / sizeof(E);
   const int lane = static_cast<int>(threadIdx.x) & 63, chunk = lane & (lanes - 1), sub = lane / lanes, abreast = 64 / lanes, D = a.cache.dim, H = a.cache.heads;
   const int h0 = blockIdx.y * heads_per_block, h1 = min(2 * H, h0 + heads_per_block);   // keys, then values
   const int page_shift = __builtin_ctz(a.cache.page_size);
@@ -232,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
       count = min(step, count - k * step);
     }
     const long r = r0 + sub;
-    if (chunk * 8 >= D || r >= a.rows) continue;
+    if (chunk * N >= D || r >= a.rows) continue;
     long begin = a.row_start[b], end = a.row_start[b + 1];
     while (r >= end && b + 1 < a.B) {
       begin = end;
@@ -243,10 +258,10 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
     int page = t >= 0 && t < held ? a.block_table[static_cast<long>(b) * a.max_pages + (t >> page_shift)] : -1;
     if (page >= a.cache.pages) page = -1;
     const int at = static_cast<int>(t & (a.cache.page_size - 1));
-    const long place = page * a.cache.page_stride + static_cast<long>(at) * D + chunk * 8;
+    const long place = page * a.cache.page_stride + static_cast<long>(at) * D + chunk * N;
     const long scale_place = page * a.cache.scale_page_stride + static_cast<long>(at) * (D / 32) + chunk / 4;
     for (int h = h0; h < h1; h += kAtOnce) {
-      Eight<E> x[kAtOnce];
+      Piece<E, N> x[kAtOnce];
       u32x2 code[kAtOnce];
       uint32_t scale[kAtOnce];
 #pragma unroll
@@ -263,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
             scale[u] = static_cast<const uint8_t*>(is_v ? a.cache.v_scales : a.cache.k_scales)[scale_place + head * (D / 32)];
           }
         } else {
-          const float z[8] = {};
+          const float z[N] = {};
           x[u].set(z);
           if (page >= 0) x[u].load(static_cast<const E*>(base) + place + head * D);
         }
@@ -272,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
       for (int u = 0; u < kAtOnce; ++u) {
         if (h + u >= h1) break;
         const bool is_v = h + u >= H;
-        if (KIND == MOE_MX8) {
+        if constexpr (KIND == MOE_MX8) {
           // 2^(s - 127); s = 0 is the subnormal 2^-127.  A code times it fits bf16 whole unless it falls below bf16's smallest numbers.
           const float sc = scale[u] != 0u ? __uint_as_float(scale[u] << 23) : __uint_as_float(0x00400000u);
           float v[8];
@@ -284,14 +299,14 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
           x[u].set(v);
         }
         E* dst = static_cast<E*>(is_v ? a.v_out : a.k_out);
-        x[u].store(dst + (r * H + (is_v ? h + u - H : h + u)) * D + chunk * 8);
+        x[u].store(dst + (r * H + (is_v ? h + u - H : h + u)) * D + chunk * N);
       }
     }
   }
 }
 
 template <int KIND> void launch_read(const CacheReadArgs& a) {
-  const int lanes = lanes_of_row(a.cache.dim), per_block = kWaves * (64 / lanes), heads = 2 * a.cache.heads;
+  const int lanes = lanes_of_row(a.cache.dim, KIND == MOE_F32 ? 4 : 8), per_block = kWaves * (64 / lanes), heads = 2 * a.cache.heads;
   const int bx = a.rows / per_block + (a.rows % per_block != 0), gx = bx < kMaxBlocksX ? bx : kMaxBlocksX;
   const int want = ceil_div(kBlocksWanted, gx), most = ceil_div(heads, kAtOnce), cut = want < most ? want : most;
   const int hpb = ceil_div(ceil_div(heads, cut), kAtOnce) * kAtOnce;
@@ -341,7 +356,9 @@ int32_t rope(const char* who, const char* name, int back, const void* q, int64_t
   a.interleaved = interleaved != 0; a.back = back; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.k_out = k_out; a.ko_stride_t = ko_stride_t; a.ko_stride_h = ko_stride_h; a.stream = static_cast<hipStream_t>(stream);
   begin_call(who, a.stream);
-  if (dtype == MOE_BF16) launch_rotate<bf16_t, 0>(name, a); else launch_rotate<float, 0>(name, a);
+  if (dtype == MOE_BF16) launch_rotate<bf16_t, 8, 0>(name, a);
+  else if (D <= 256) launch_rotate<float, 4, 0>(name, a);
+  else launch_rotate<float, 8, 0>(name, a);
   return end_call();
 }
 
@@ -426,9 +443,9 @@ extern "C" int32_t moe_kv_cache_write(const moe_kv_cache_t* cache, const void* k
   a.interleaved = interleaved != 0; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.slots = slots; a.cache = *cache; a.stream = static_cast<hipStream_t>(stream);
   begin_call("moe_kv_cache_write", a.stream);
-  if (cache->dtype == MOE_F32) launch_rotate<float, 1>("kv_cache_write", a);
-  else if (cache->dtype == MOE_BF16) launch_rotate<bf16_t, 1>("kv_cache_write", a);
-  else launch_rotate<bf16_t, 2>("kv_cache_write", a);
+  if (cache->dtype == MOE_F32) launch_rotate<float, 4, 1>("kv_cache_write", a);
+  else if (cache->dtype == MOE_BF16) launch_rotate<bf16_t, 8, 1>("kv_cache_write", a);
+  else launch_rotate<bf16_t, 8, 2>("kv_cache_write", a);
   return end_call();
 }
 
