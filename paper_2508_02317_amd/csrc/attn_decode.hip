@@ -127,7 +127,7 @@ template <int N> struct ScaleRow {
 template <int KIND, int D> struct Wave {
   static constexpr bool kF32 = KIND == MOE_F32, kMx = KIND == MOE_MX8;
   static constexpr int kHalves = attn_halves(KIND, D), kSub = 16 * kHalves, kStep = kWaves * kSub;   // tokens of a wave, of a workgroup at a time
-  static constexpr int kG = D % 128 == 0 ? 128 : 64, kE = kG / 16, kNG = D / kG;   // a lane's values: kE elements of each of kNG groups of kG
+  static constexpr int kG = !kF32 && D % 128 == 0 ? 128 : 64, kE = kG / 16, kNG = D / kG;   // a lane's values: kE elements of each of kNG groups of kG
   static constexpr int kEs = kF32 ? 4 : kMx ? 1 : 2, kRow = D * kEs;               // bytes of an element, of a token's row
   static constexpr int kKPieces = kMx ? D / 64 : kF32 ? D / 16 : D / 32;           // 16-byte pieces of a key row that a lane reads
   static constexpr int kKStep = 64;                                                // bytes between them (4 lanes of 16 bytes)
@@ -646,7 +646,8 @@ Launch launch_of(int dtype, int dim, int B, int Hq, int Hkv, int page_size, int 
   l.tile_subs = l.cut ? kWaves : static_cast<int>(subs < 1 ? 1 : subs);
   l.most_subs = subs * units;
   const int64_t most = (l.cut ? (subs + kWaves - 1) / kWaves : 1) * units;
-  l.blocks = static_cast<int>(most < kAttnMaxBlocks ? most : kAttnMaxBlocks);
+  const int at_once = dim > 128 ? kAttnMaxBlocks / 2 : kAttnMaxBlocks;   // as many as the card has room for: one or two a CU
+  l.blocks = static_cast<int>(most < at_once ? most : at_once);
   if (l.blocks < 1) l.blocks = 1;
   return l;
 }
