@@ -103,6 +103,7 @@ template <int N> struct Words {
     for (int i = 0; i < N / kLanes; ++i) w[i] = rows.template load<V, AUX>(off + i * static_cast<int>(sizeof(V)));
   }
   __device__ __forceinline__ uint32_t operator[](int i) const { return w[i / kLanes][i % kLanes]; }
+  __device__ __forceinline__ void put(int i, uint32_t x) { w[i / kLanes][i % kLanes] = x; }
 };
 
 // N bytes that begin at a multiple of N: whole words where N is one, else pairs of bytes.
@@ -247,18 +248,36 @@ template <int KIND, int D> struct Wave {
         l += s[a][r];
       }
   }
-  // out += values * p; `mask`: bit 4 a + r set where this lane's token exists (used where CUT)
-  template <bool CUT> __device__ __forceinline__ void output(const f32x4 (&p)[kHalves], uint32_t mask, int n) {
+  // Values of tokens that do not exist become zeros: their p is 0, but what lies there may be infinite or NaN.
+  __device__ __forceinline__ void clear_missing(uint32_t mask) {
+#pragma unroll
+    for (int t = 0; t < kVTokens; ++t) {
+      const bool there = (mask >> t) & 1u;
+#pragma unroll
+      for (int g = 0; g < kNG; ++g)
+#pragma unroll
+        for (int i = 0; i < kVWords; ++i) v[t][g].put(i, there ? v[t][g][i] : 0u);
+      if constexpr (kMx) {                             // and the scales: a scale code of 255 stands for NaN
+#pragma unroll
+        for (int i = 0; i < kScaleRow; ++i) {          // word i of the four tokens' bytes
+          uint32_t bytes = 0u;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) bytes |= (4 * i + b) / kScaleRow == t % 4 ? 0xFFu << (8 * b) : 0u;
+          if (bytes != 0u) vs[t / 4].put(i, there ? vs[t / 4][i] : vs[t / 4][i] & ~bytes);
+        }
+      }
+    }
+  }
+  // out += values * p
+  __device__ __forceinline__ void output(const f32x4 (&p)[kHalves], int n) {
     if constexpr (kF32) {
 #pragma unroll
       for (int r = 0; r < kVTokens; ++r)
 #pragma unroll
         for (int g = 0; g < kNG; ++g)
 #pragma unroll
-          for (int e = 0; e < kE; ++e) {
-            const float x = CUT && !((mask >> r) & 1u) ? 0.0f : __uint_as_float(v[r][g][e]);
-            acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[r / 4][r % 4], acc[g][e], 0, 0, 0);
-          }
+          for (int e = 0; e < kE; ++e)
+            acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][g][e]), p[r / 4][r % 4], acc[g][e], 0, 0, 0);
     } else {
 #pragma unroll
      for (int two = 0; two < kHalves; two += 2) {
@@ -287,10 +306,6 @@ template <int KIND, int D> struct Wave {
           } else {
 #pragma unroll
             for (int e = 0; e < kE / 2; ++e) w[t][e] = v[vt][g][e];
-          }
-          if constexpr (CUT) {
-#pragma unroll
-            for (int e = 0; e < kE / 2; ++e) w[t][e] = (mask >> vt) & 1u ? w[t][e] : 0u;
           }
         }
 #pragma unroll
@@ -490,7 +505,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
           }
       }
       w.softmax(s, a.scale_hi, a.scale_lo, mask);
-      if (whole) w.template output<false>(s, mask, n); else w.template output<true>(s, mask, n);
+      if (!whole) w.clear_missing(mask);
+      w.output(s, n);
       load_v(from, t1);
       t0 = t1;
     }
