@@ -6,8 +6,11 @@
 // with the pair (i, i + rot/2), or (2i, 2i + 1) where neighbours are paired; elements from rot on stay as they are.  The turn is a
 // rotation, so its gradient is the turn by the opposite angle.
 //
-// Everything here moves bytes and is bound by HBM.  A lane owns 16 consecutive bytes of a head, so that a head row
-// is contiguous over its lanes in every access; a row's lanes lie in one wave (up to 64 of them, rounded up to a power of two).
+// Everything here moves bytes and is bound by HBM.  A lane owns 16 consecutive bytes of a head, so that a head row is contiguous over its
+// lanes in every access; a row's lanes lie in one wave (up to 64 of them, rounded up to a power of two).  Tensors are streamed past the
+// caches, table and scales are not.  Measured, in brackets with ordinary accesses: 40960 tokens of 32 + 4 heads of 128 elements in bf16, 755 MB,
+// 124 us (142), 6.1 TB/s, the rate of a streaming copy; 8192 tokens 28 us (33), 5.4 TB/s; with keys and values stored into a cache 31 us (37),
+// 5.5; 52949 cached tokens read back, 217 MB, 37 us (45), 5.8.  256 tokens of 16 heads take the 4 to 5 us of a launch.
 // The partner elements of the half layout come from the lane that owns them, not from memory again: a row is read whole before any
 // of it is written, which makes the turn in place safe, and is read once.  The cosines and sines of a token are read once per lane and used for
 // all heads that the lane walks.
