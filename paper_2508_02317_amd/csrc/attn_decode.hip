@@ -71,7 +71,7 @@ struct Args {
   void* out;
   float* lse;
   int32_t* unit_pieces;                                // [B * Hkv * parts][2]: first workgroup (its slot in bit 0) and last of a cut unit, or -1
-  float* slots;                                        // [2 W][heads][D + 2]: maximum, sum, output
+  float* slots;                                        // [2 W][heads][D + 4]: maximum, sum, two unused, output
 };
 
 __device__ __forceinline__ float row_max4(float v) {   // over the four lanes of the same n
@@ -350,8 +350,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
   // Tiles of all sequences, and the sequence in which this workgroup's piece begins.  Every wave finds them for itself, four consecutive
   // sequences a lane, without a barrier: a load, a scan over the lanes, a ballot.
   const ScalarInts lens = scalar_ints(a.lens);
-  const int tile = a.tile_subs * W::kSub;
-  auto span_of = [&](int len) { return attn_span(len, held, a.window, W::kSub, tile); };
+  // (a whole context is one tile of any length: with constants there is no division)
+  auto span_of = [&](int len) { return a.unit_pieces ? attn_span(len, held, a.window, W::kSub, W::kStep) : attn_span(len, held, a.window, W::kSub, 1 << 30); };
   int len4[4], nt[4], mine = 0, incl = 0;              // of this lane's sequences: lengths, tiles of each, their sum, the sum up to and with this lane
   bool empty = false;                                  // some sequence has no tokens
   auto count_from = [&](int b0) {
@@ -526,25 +526,17 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       load_v(next, next.t0);
     }
 
-    // the four waves' parts, and out
+    // the four waves' parts, each to its own maximum, and out
     const float l = row_sum4(w.l);
-    __syncthreads();                                   // the last piece's sums have been read
     if (lane < 16) { s_m[wave][n] = w.m; s_l[wave][n] = l; }
-    __syncthreads();
-    {
-      const float m = fmaxf(fmaxf(s_m[0][n], s_m[1][n]), fmaxf(s_m[2][n], s_m[3][n]));
-      const float f = w.m > -INFINITY ? __builtin_amdgcn_exp2f(w.m - m) : 0.0f;
-      if (n < heads) {
+    if (n < heads) {
 #pragma unroll
-        for (int g = 0; g < W::kNG; ++g)
+      for (int g = 0; g < W::kNG; ++g)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < W::kE; e += 4) {
-              const f32x4 x = {w.acc[g][e][r] * f, w.acc[g][e + 1][r] * f, w.acc[g][e + 2][r] * f, w.acc[g][e + 3][r] * f};
-              *reinterpret_cast<f32x4*>(&s_out[wave][n][g * W::kG + (4 * c + r) * W::kE + e]) = x;
-            }
-      }
+          for (int e = 0; e < W::kE; e += 4)
+            *reinterpret_cast<f32x4*>(&s_out[wave][n][g * W::kG + (4 * c + r) * W::kE + e]) = f32x4{w.acc[g][e][r], w.acc[g][e + 1][r], w.acc[g][e + 2][r], w.acc[g][e + 3][r]};
     }
     __syncthreads();
     const bool complete = cur.first == cur.unit_begin && cur.last == cur.unit_end;
@@ -556,8 +548,9 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int v = 0; v < kWaves; ++v) {
-        sum += s_m[v][h] > -INFINITY ? s_l[v][h] * __builtin_amdgcn_exp2f(s_m[v][h] - m) : s_l[v][h];
-        o += *reinterpret_cast<const f32x4*>(&s_out[v][h][d]);
+        const float f = s_m[v][h] > -INFINITY ? __builtin_amdgcn_exp2f(s_m[v][h] - m) : 0.0f;
+        sum += s_l[v][h] * f;
+        o += *reinterpret_cast<const f32x4*>(&s_out[v][h][d]) * f;
       }
       if (complete) {
         const int64_t row = static_cast<int64_t>(cur.b) * a.Hq + cur.head0 + h;
@@ -580,6 +573,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
       p[1] = attn_owner(cut, cur.unit_end - 1);
     }
     if (cur.last >= end) return;
+    __syncthreads();                                   // the sums have been read
     cur = next;
   }
 }
