@@ -659,7 +659,7 @@ Launch launch_of(int dtype, int dim, int B, int Hq, int Hkv, int page_size, int 
   l.parts = ceil_div(group, 16);
   l.heads = ceil_div(group, l.parts);
   const int64_t units = static_cast<int64_t>(B) * Hkv * l.parts, held = static_cast<int64_t>(page_size) * max_pages;
-  const int64_t seen = window > 0 && window + l.sub < held ? window + l.sub : held, subs = (seen + l.sub - 1) / l.sub;   // a window may begin inside a stretch
+  const int64_t most_seen = static_cast<int64_t>(window) + l.sub, seen = window > 0 && most_seen < held ? most_seen : held, subs = (seen + l.sub - 1) / l.sub;   // a window may begin inside a stretch
   // A context of few stretches is not cut (its one tile is the whole): a workgroup has it in a few turns, and no second launch is needed.
   // 4 key heads of 128 elements in bf16, cut -> whole: one context of 250 tokens 11.1 -> 7.9 us, 500 10.8 -> 9.5, 1000 10.8 -> 14.4; 64 contexts of
   // 250 14.4 -> 10.2, 500 18.4 -> 14.6, 1000 27.2 -> 23.6; 512 of 250 63 -> 54, 1000 180 -> 173.

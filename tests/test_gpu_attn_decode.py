@@ -223,3 +223,14 @@ def test_a_generation_step_replays_from_a_graph():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ref, (q_out, out, lse, cache.k, cache.k_scales))), rep
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 32, 2 ** 31 - 33, 2 ** 30])
+def test_a_window_beyond_every_context_is_none(window):
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    say("attend, window %d" % window)
+    cache, q, table, n = build("bf16", [2500, 3, 0, 700], 8, 2, 128, 16, 8)
+    dev = to_dev(table), to_dev(n)
+    a, b = (L.moe_paged_attn_decode(q, cache, *dev, window=w, lse=True) for w in (0, window))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
