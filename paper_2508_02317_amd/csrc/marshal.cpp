@@ -67,8 +67,10 @@ struct Heads {
     const at::Tensor& t = tensor(o, name);
     if (t.dim() != 3 || !t.is_cuda()) refuse(PyExc_ValueError, "%s must be a [tokens, heads, dim] device tensor", name);
     if (t.stride(2) != 1 && t.size(2) != 1) refuse(PyExc_ValueError, "%s: the elements of a head must be contiguous", name);
-    p = t.data_ptr(); st = t.stride(0); sh = t.stride(1);
+    p = t.data_ptr();
     tokens = size32(t, 0); heads = size32(t, 1); dim = size32(t, 2);
+    st = tokens > 1 ? t.stride(0) : 0;                 // the stride of one token or one head is never taken
+    sh = heads > 1 ? t.stride(1) : 0;
     type = t.scalar_type();
   }
   void like(int T, int H, int D, at::ScalarType want, const char* name) const {

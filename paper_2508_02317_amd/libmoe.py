@@ -495,7 +495,7 @@ def _heads(t, dtype, name, shape=None):
         raise ValueError("%s: the elements of a head must be contiguous" % name)
     if shape is not None and t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    return t.data_ptr(), st[0], st[1]
+    return t.data_ptr(), st[0] if t.shape[0] > 1 else 0, st[1] if t.shape[1] > 1 else 0   # the stride of one token or one head is never taken
 
 
 _NO_HEADS = (None, 0, 0)
@@ -675,6 +675,8 @@ def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None,
         raise ValueError("out must have the shape of q")
     if lse is not None and _need(lse, torch.float32, "lse").shape != (B, Hq):
         raise ValueError("lse must be [%d, %d]" % (B, Hq))
+    if window != ctypes.c_int32(window).value:
+        raise OverflowError("window does not fit 32 bits")
     _check(lib.moe_paged_attn_decode(*qi, cache.ref, pages.data_ptr(), pages.shape[1], lens.data_ptr(), B, Hq, scale, window, out.data_ptr(), _ptr(lse),
                                      ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
     return out, lse

@@ -142,3 +142,31 @@ def test_refusals_of_the_binding(compiled, monkeypatch):
                 (mk(3, 16, 1, 64).transpose(1, 2), mk(3, 1, 16, 64)), (mk(3, 1, 16, 64), mk(3, 1, 16, 64), mk(3, 1, 16, 2, t=torch.uint8))):
         with pytest.raises(ValueError):
             L.moe_kv_cache(*bad)
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+def test_one_token_or_one_head_has_no_stride(compiled, monkeypatch):
+    """A view's stride over one token or one head is never taken, so it may be anything."""
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    if compiled and L._marshal is None:
+        pytest.skip("_marshal.so is not built here")
+    if not compiled:
+        monkeypatch.setattr(L, "_marshal", None)
+    x = torch.randn((8 * 67 * 3,), device="cuda").bfloat16()
+    view = lambda T, H, st, sh: x.as_strided((T, H, 64), (st, sh, 1))
+    pos = torch.arange(4, dtype=torch.int32, device="cuda")
+    cos, sin = L.moe_rope_table(torch.ones(32, dtype=torch.float64, device="cuda"), 8)
+    cache = L.moe_kv_cache(*(torch.zeros((2, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    table, lens = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    for T, H, st, sh in ((1, 3, 67, 72), (4, 1, 72, 67), (1, 1, 3, 5)):
+        q, k = view(T, H, st, sh), view(T, 1, 72 if T > 1 else 67, 67)
+        ref = L.moe_rope_fwd(q.contiguous(), k.contiguous(), pos[:T], cos, sin)
+        got = L.moe_rope_fwd(q, k, pos[:T], cos, sin)
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+        q_out = L.moe_kv_cache_write(cache, k, k, pos[:T].long(), q, pos[:T], cos, sin)
+        assert torch.equal(q_out, ref[0]) and torch.equal(cache.k[0, 0, :T], ref[1][:, 0]) and torch.equal(cache.v[0, 0, :T], k[:, 0])
+        out, _ = L.moe_paged_attn_decode(q[:1], cache, table, lens)
+        assert torch.equal(out[0], k[0].expand(H, 64))
+    with pytest.raises(OverflowError):
+        L.moe_paged_attn_decode(q[:1], cache, table, lens, window=2 ** 32 + 1)
