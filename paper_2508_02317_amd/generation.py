@@ -78,9 +78,11 @@ class PagedKVCache:
 
     def grow(self, seqs, counts):
         """Places for counts[i] new tokens of seqs[i] -> slots [sum] i64, positions [sum] i32, pages [B, widest] i32, lens [B] i32, all on
-        the device.  Nothing changes where the free pages do not suffice (MemoryError)."""
+        the device.  Nothing changes where the arguments do not fit (ValueError) or the free pages do not suffice (MemoryError)."""
         if len(set(seqs)) != len(seqs):
             raise ValueError("a sequence is named twice")
+        if len(counts) != len(seqs) or min(counts, default=0) < 0:
+            raise ValueError("every sequence needs a number of new tokens of 0 or more")
         ps = self.page_size
         need = [-(-(self.length[s] + n) // ps) - len(self.pages_of[s]) for s, n in zip(seqs, counts)]
         if sum(max(n, 0) for n in need) > len(self.free):
@@ -109,26 +111,28 @@ class CachedAttention:
         if w_qkv.shape[0] != (heads + 2 * self.kv_heads) * self.dim or w_out.shape[1] != heads * self.dim:
             raise ValueError("w_qkv must have (heads + 2 kv_heads) dim rows and w_out heads dim columns")
 
-    def _project(self, x, slots, positions):
-        """Keys and values of the rows of x into the cache; -> their rotated queries [T, heads, dim], a view of the projection's output."""
-        if len(positions) and self.cos.shape[0] < max(self.cache.length.values()):
+    def _grow(self, x, seqs, counts):
+        """Room for the rows of x, and their keys and values in the cache; -> their rotated queries [T, heads, dim], a view of the projection's output,
+        with the pages and lengths of the sequences.  What does not fit is refused before a sequence has grown."""
+        if len(x) != sum(counts):
+            raise ValueError("%d rows for %d new tokens" % (len(x), sum(counts)))
+        if max((self.cache.length[s] + n for s, n in zip(seqs, counts)), default=0) > self.cos.shape[0]:
             raise ValueError("the rotation table ends at position %d" % self.cos.shape[0])
-        qkv = torch.mm(x, self.w_qkv.t()).view(len(x), -1, self.dim)
+        slots, positions, pages, lens = self.cache.grow(seqs, counts)
+        qkv = torch.mm(x, self.w_qkv.t()).view(len(x), self.heads + 2 * self.kv_heads, self.dim)
         q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
-        return L.moe_kv_cache_write(self.cache.view, k, v, slots, q, positions, self.cos, self.sin, self.interleaved, q_out=q)
+        return L.moe_kv_cache_write(self.cache.view, k, v, slots, q, positions, self.cos, self.sin, self.interleaved, q_out=q), pages, lens
 
     def token(self, x, seqs):
         """One new token x[i] of every sequence seqs[i] -> [B, d]."""
-        slots, positions, pages, lens = self.cache.grow(seqs, [1] * len(seqs))
-        q = self._project(x, slots, positions)
+        q, pages, lens = self._grow(x, seqs, [1] * len(seqs))
         y, _ = L.moe_paged_attn_decode(q, self.cache.view, pages, lens, window=self.window)
-        return torch.mm(y.view(len(x), -1), self.w_out.t())
+        return torch.mm(y.view(len(x), self.heads * self.dim), self.w_out.t())
 
     def prompt(self, x, seqs, counts):
         """counts[i] new tokens of seqs[i], their rows of x one sequence after the other -> [sum(counts), d].  Every token attends to what its
         sequence has in the cache up to itself."""
-        slots, positions, pages, lens = self.cache.grow(seqs, counts)
-        q = self._project(x, slots, positions)
+        q, pages, _ = self._grow(x, seqs, counts)
         ends = [self.cache.length[s] for s in seqs]
         starts = torch.tensor([0] + ends, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(x.device)
         k, v = L.moe_kv_cache_read(self.cache.view, pages, starts, rows=sum(ends))
@@ -142,4 +146,4 @@ class CachedAttention:
             hidden = (t > own) | (t <= own - self.window) if self.window else t > own
             y[row:row + n] = (score.masked_fill(hidden, -math.inf).softmax(-1) @ vv).transpose(0, 1).to(y.dtype)
             row, key = row + n, key + end
-        return torch.mm(y.view(len(x), -1), self.w_out.t())
+        return torch.mm(y.view(len(x), self.heads * self.dim), self.w_out.t())

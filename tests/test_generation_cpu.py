@@ -54,3 +54,29 @@ def test_pages_are_handed_out_and_taken_back(cache):
         cache.grow(["b", "b"], [1, 1])
     cache.close("b")
     assert sorted(cache.free) == list(range(6))
+
+
+def test_counts_that_do_not_fit_change_nothing(cache):
+    cache.open("a"); cache.open("b")
+    cache.grow(["a", "b"], [5, 20])
+    before = dict(cache.length), {s: list(p) for s, p in cache.pages_of.items()}, list(cache.free)
+    for counts in ([1], [1, 1, 1], [3, -1]):
+        with pytest.raises(ValueError):
+            cache.grow(["a", "b"], counts)
+        assert before == (cache.length, cache.pages_of, cache.free)
+    assert [len(t) for t in cache.grow([], [])] == [0, 0, 0, 0]
+
+
+def test_rows_that_do_not_fit_leave_the_sequences_as_they_were(cache):
+    cache.view = type("View", (), dict(heads=2, dim=64))
+    w = torch.zeros((4 + 4) * 64, 32)
+    cos = torch.zeros(40, 32)
+    attention = G.CachedAttention(cache, 4, w, torch.zeros(32, 4 * 64), cos, cos)
+    cache.open("a"); cache.open("b")
+    cache.grow(["a", "b"], [40, 3])
+    before = dict(cache.length), list(cache.free)
+    for call in (lambda: attention.token(torch.zeros(1, 32), ["a"]), lambda: attention.prompt(torch.zeros(39, 32), ["b"], [39]),     # past the table
+                 lambda: attention.token(torch.zeros(2, 32), ["b"]), lambda: attention.prompt(torch.zeros(3, 32), ["b"], [4])):          # not as many rows
+        with pytest.raises(ValueError):
+            call()
+        assert before == (cache.length, cache.free)

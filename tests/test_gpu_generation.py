@@ -170,3 +170,16 @@ def test_one_token_or_one_head_has_no_stride(compiled, monkeypatch):
         assert torch.equal(out[0], k[0].expand(H, 64))
     with pytest.raises(OverflowError):
         L.moe_paged_attn_decode(q[:1], cache, table, lens, window=2 ** 32 + 1)
+
+
+def test_steps_of_no_sequences_and_chunks_of_no_tokens():
+    import torch
+    generate, block = block_of(True, base=1e4)
+    none = torch.empty((0, 256), dtype=torch.bfloat16, device="cuda")
+    assert block.attention.token(none, []).shape == (0, 256) and block.attention.prompt(none, [], []).shape == (0, 256)
+    block.cache.open(0); block.cache.open(1)
+    assert block.attention.prompt(none, [0, 1], [0, 0]).shape == (0, 256)
+    x = torch.randn((21, 256), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda").bfloat16()
+    y = block.attention.prompt(x, [0, 1], [0, 21])                   # one of them has something to say
+    block.cache.open(2)
+    assert torch.equal(y, block.attention.prompt(x, [2], [21])) and block.cache.length == {0: 0, 1: 21, 2: 21}
