@@ -360,6 +360,7 @@ int32_t moe_kv_cache_read(const moe_kv_cache_t* cache, const int32_t* block_tabl
  *   q [B, Hq, dim] (strides q_stride_b, q_stride_h, multiples of 16 bytes), out [B, Hq, dim] dense, both f32 for an MOE_F32 cache, else bf16;
  *   lse [B, Hq] f32 or NULL: the natural logarithm of the sum of exp(score), with which results over parts of a context are joined.
  *   A sequence without tokens gets zeros and lse = -inf.  Places of the cache outside a sequence's tokens may hold anything.
+ *   A value of theirs that is infinite or NaN makes the same element of its heads' outputs infinite or NaN, and no other.
  *   Scores, softmax and sums are fp32; the result is rounded once.  Page ids are taken as the nearest that exists.
  *   The order of the sums depends on lens, B and the sizes only: the same call gives the same bits.
  *   Hq a multiple of heads; B * heads * context length up to 2^31 or so (MOE_ERR_UNSUPPORTED beyond).

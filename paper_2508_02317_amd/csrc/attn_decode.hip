@@ -26,14 +26,15 @@
 //     two of them, and a second launch joins those.  The cut depends on lens alone, so results do not change from call to call.  Tiles of kSub tokens
 //     would cut more evenly but leave three waves of four idle in a workgroup's last round: 16 contexts of up to 4096 tokens 24 -> 29.5 us.
 //     512 workgroups (256 of more than 128 elements) are what the card has room for; 768 and 1024 were 2 to 8 % slower.
+//     Eight waves on half as many workgroups: 64 contexts of 8192 tokens 1 to 3 % faster, one of 100 to 1000 15 to 20 % slower.
 //
 // Scores are fp32 sums of exact products (8-bit values are exact in bf16).  p is split into two bf16 numbers, together exact to 2^-16, so that
 // rounding it leaves the result as if it had not been rounded; one alone made the error against 64 bits 1.01 to 1.04 times as large, and the second
 // product takes nothing in bf16 and up to 2 % with an 8-bit cache.
 //
 // Measured on one MI355X, both launches: 128 contexts of 8192 tokens (4 key heads of 128 elements, 32 query heads, bf16, 2.1 GB) 320 us, 6.8 TB/s
-// in the first launch, where a kernel that reads and does nothing else has 7.0; 64 contexts of up to 8192, 548 MB, 95 to 98 us; 32 of up to
-// 40960 in 8 bits, 702 MB, 119 to 124 us (5.9 TB/s: the vector unit is busy a third of the time, the matrix unit an eighth).  What is missing on shorter
+// in the first launch, where a kernel that reads and does nothing else has 7.0; 64 contexts of up to 8192, 548 MB, 94 to 97 us; 32 of up to
+// 40960 in 8 bits, 702 MB, 119 to 124 us (5.9 TB/s: the vector unit is busy four tenths of the time, the matrix unit an eighth).  What is missing on shorter
 // calls is fixed: about 5 us from the launch to the first keys (arguments, lengths, page ids and keys, each waited for by the next), 3 at the
 // end and 3 to 5 for the join.
 #include <cmath>

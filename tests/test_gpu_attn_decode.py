@@ -234,3 +234,20 @@ def test_a_window_beyond_every_context_is_none(window):
     dev = to_dev(table), to_dev(n)
     a, b = (L.moe_paged_attn_decode(q, cache, *dev, window=w, lse=True) for w in (0, window))
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[400, 90], [20, 3000]])
+def test_infinite_and_not_a_number_values_where_they_count(kind, lens):
+    """They make their element of their heads' outputs infinite or NaN, and leave every other as it is."""
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    cache, q, table, n = build(kind, lens, 4, 2, 64, 16, 9)
+    dev = to_dev(table), to_dev(n)
+    ref, ref_lse = L.moe_paged_attn_decode(q, cache, *dev, lse=True)
+    cache.v[int(table[0, 1]), 0, 2, 7] = float("inf")                # first context, token 18: heads 0 and 1
+    cache.v[int(table[1, 0]), 1, 3, 60] = float("nan")               # second context, token 3: heads 2 and 3
+    out, lse = L.moe_paged_attn_decode(q, cache, *dev, lse=True)
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[0, :2, 7] = hit[1, 2:, 60] = True
+    assert torch.equal(lse, ref_lse) and not torch.isfinite(out[hit]).any() and torch.equal(out[~hit], ref[~hit])
