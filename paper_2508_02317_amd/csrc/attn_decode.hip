@@ -423,20 +423,20 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
     }
     Part q;
     q.b = b_at;
-    q.u = (tile - before * units) / sp.tiles;
+    q.u = quotient(tile - before * units, sp.tiles);
     q.unit_begin = before * units + q.u * sp.tiles;
     q.unit_end = q.unit_begin + sp.tiles;
     q.first = tile;
     q.last = min(end, q.unit_end);
-    q.kv = q.u / a.parts;
+    q.kv = a.parts == 1 ? q.u : quotient(q.u, a.parts);
     const int part = q.u - q.kv * a.parts;
     q.head0 = q.kv * a.group + part * a.heads;
     q.heads = min(a.heads, a.group - part * a.heads);
     q.lo = sp.lo;
     q.len = sp.len;
-    const int sub0 = (tile - q.unit_begin) * a.tile_subs + wave, sub1 = min((q.last - q.unit_begin) * a.tile_subs, (sp.len - sp.base + W::kSub - 1) / W::kSub);
+    const int sub0 = (tile - q.unit_begin) * a.tile_subs + wave, sub1 = min((q.last - q.unit_begin) * a.tile_subs, quotient(sp.len - sp.base + W::kSub - 1, W::kSub));
     q.t0 = sp.base + sub0 * W::kSub;
-    q.rounds = sub0 < sub1 ? (sub1 - sub0 + kWaves - 1) / kWaves : 0;
+    q.rounds = sub0 < sub1 ? quotient(sub1 - sub0 + kWaves - 1, kWaves) : 0;
     q.until = sub0 < sub1 ? min(sp.len, sp.base + sub1 * W::kSub) : 0;
     q.pages = scalar_ints(a.block_table + static_cast<int64_t>(b_at) * a.max_pages);
     return q;
