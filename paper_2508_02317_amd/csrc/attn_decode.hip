@@ -491,7 +491,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void attn_decode_kernel(
     if (cur.last < end) next = part_at(cur.last);
     const int lo = cur.lo, len = cur.len, heads = cur.heads;
     w.take_q();
-    load_q(next);
+    if (cur.last < end) load_q(next);
     w.begin();
     int t0 = cur.t0;
     if (cur.rounds > 1) find_pages(cur, t0 + W::kStep); else find_pages(next, next.t0);
