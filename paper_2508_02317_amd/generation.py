@@ -85,8 +85,8 @@ class PagedKVCache:
             raise ValueError("every sequence needs a number of new tokens of 0 or more")
         ps = self.page_size
         need = [-(-(self.length[s] + n) // ps) - len(self.pages_of[s]) for s, n in zip(seqs, counts)]
-        if sum(max(n, 0) for n in need) > len(self.free):
-            raise MemoryError("%d pages wanted, %d free" % (sum(max(n, 0) for n in need), len(self.free)))
+        if sum(need) > len(self.free):
+            raise MemoryError("%d pages wanted, %d free" % (sum(need), len(self.free)))
         slots, positions = [], []
         for s, n, new in zip(seqs, counts, need):
             mine, at = self.pages_of[s], self.length[s]
@@ -98,7 +98,21 @@ class PagedKVCache:
         table = [p for s in seqs for p in self.pages_of[s] + [0] * (widest - len(self.pages_of[s]))]
         lens = [self.length[s] for s in seqs]
         to = lambda v, t: torch.tensor(v, dtype=t).to(self.device)
-        return to(slots, torch.int64), to(positions, torch.int32), to(table, torch.int32).view(len(seqs), widest), to(lens, torch.int32)
+        try:
+            return to(slots, torch.int64), to(positions, torch.int32), to(table, torch.int32).view(len(seqs), widest), to(lens, torch.int32)
+        except BaseException:                          # no memory on the device
+            self.shrink(seqs, counts)
+            raise
+
+    def shrink(self, seqs, counts):
+        """Takes the last counts[i] tokens of seqs[i] back, and the pages that held nothing else: after a grow of the same arguments everything, the
+        order of the free pages included, is as it was before.  Nothing changes where the arguments do not fit (ValueError)."""
+        if len(set(seqs)) != len(seqs) or len(counts) != len(seqs) or not all(0 <= n <= self.length[s] for s, n in zip(seqs, counts)):
+            raise ValueError("every sequence needs a number of tokens that it has")
+        for s, n in zip(reversed(seqs), reversed(counts)):
+            self.length[s] -= n
+            while len(self.pages_of[s]) > -(-self.length[s] // self.page_size):
+                self.free.append(self.pages_of[s].pop())
 
 
 class CachedAttention:
@@ -111,39 +125,47 @@ class CachedAttention:
         if w_qkv.shape[0] != (heads + 2 * self.kv_heads) * self.dim or w_out.shape[1] != heads * self.dim:
             raise ValueError("w_qkv must have (heads + 2 kv_heads) dim rows and w_out heads dim columns")
 
-    def _grow(self, x, seqs, counts):
-        """Room for the rows of x, and their keys and values in the cache; -> their rotated queries [T, heads, dim], a view of the projection's output,
-        with the pages and lengths of the sequences.  What does not fit is refused before a sequence has grown."""
-        if len(x) != sum(counts):
-            raise ValueError("%d rows for %d new tokens" % (len(x), sum(counts)))
+    def _step(self, x, seqs, counts, attend):
+        """Projections around attend(q, pages, lens) -> [T, heads, dim] with the rows of x stored: q their rotated queries [T, heads, dim], a view of the
+        projection's output, pages and lens those of the sequences.  What does not fit is refused before a sequence has grown, and where anything
+        raises after that (memory that runs out, a call that refuses), the growth is taken back: no sequence keeps places that were not written."""
+        d = self.w_qkv.shape[1]
+        if x.dim() != 2 or x.shape[1] != d or len(x) != sum(counts):
+            raise ValueError("rows of %d elements for %d new tokens are wanted, got %s" % (d, sum(counts), tuple(x.shape)))
+        if x.dtype is not self.w_qkv.dtype or x.device != self.w_qkv.device:
+            raise TypeError("rows must be %s on %s like the weights, got %s on %s" % (self.w_qkv.dtype, self.w_qkv.device, x.dtype, x.device))
         if max((self.cache.length[s] + n for s, n in zip(seqs, counts)), default=0) > self.cos.shape[0]:
             raise ValueError("the rotation table ends at position %d" % self.cos.shape[0])
         slots, positions, pages, lens = self.cache.grow(seqs, counts)
-        qkv = torch.mm(x, self.w_qkv.t()).view(len(x), self.heads + 2 * self.kv_heads, self.dim)
-        q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
-        return L.moe_kv_cache_write(self.cache.view, k, v, slots, q, positions, self.cos, self.sin, self.interleaved, q_out=q), pages, lens
+        try:
+            qkv = torch.mm(x, self.w_qkv.t()).view(len(x), self.heads + 2 * self.kv_heads, self.dim)
+            q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
+            q = L.moe_kv_cache_write(self.cache.view, k, v, slots, q, positions, self.cos, self.sin, self.interleaved, q_out=q)
+            return torch.mm(attend(q, pages, lens).view(len(x), self.heads * self.dim), self.w_out.t())
+        except BaseException:
+            self.cache.shrink(seqs, counts)
+            raise
 
     def token(self, x, seqs):
         """One new token x[i] of every sequence seqs[i] -> [B, d]."""
-        q, pages, lens = self._grow(x, seqs, [1] * len(seqs))
-        y, _ = L.moe_paged_attn_decode(q, self.cache.view, pages, lens, window=self.window)
-        return torch.mm(y.view(len(x), self.heads * self.dim), self.w_out.t())
+        return self._step(x, seqs, [1] * len(seqs), lambda q, pages, lens: L.moe_paged_attn_decode(q, self.cache.view, pages, lens, window=self.window)[0])
 
     def prompt(self, x, seqs, counts):
         """counts[i] new tokens of seqs[i], their rows of x one sequence after the other -> [sum(counts), d].  Every token attends to what its
         sequence has in the cache up to itself."""
-        q, pages, _ = self._grow(x, seqs, counts)
-        ends = [self.cache.length[s] for s in seqs]
-        starts = torch.tensor([0] + ends, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(x.device)
+        return self._step(x, seqs, counts, lambda q, pages, lens: self._attend_prompt(q, pages, counts, [self.cache.length[s] for s in seqs]))
+
+    def _attend_prompt(self, q, pages, counts, ends):
+        starts = torch.tensor([0] + ends, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(q.device)
         k, v = L.moe_kv_cache_read(self.cache.view, pages, starts, rows=sum(ends))
         y, row, key = torch.empty_like(q, memory_format=torch.contiguous_format), 0, 0
         for n, end in zip(counts, ends):
             g = self.heads // self.kv_heads
             kk, vv = (t[key:key + end].float().repeat_interleave(g, dim=1).transpose(0, 1).contiguous() for t in (k, v))
             score = (q[row:row + n].float().transpose(0, 1).contiguous() @ kk.transpose(1, 2).contiguous()) * self.dim ** -0.5
-            t = torch.arange(end, device=x.device)
+            t = torch.arange(end, device=q.device)
             own = t[end - n:, None]
             hidden = (t > own) | (t <= own - self.window) if self.window else t > own
             y[row:row + n] = (score.masked_fill(hidden, -math.inf).softmax(-1) @ vv).transpose(0, 1).to(y.dtype)
             row, key = row + n, key + end
-        return torch.mm(y.view(len(x), self.heads * self.dim), self.w_out.t())
+        return y

@@ -80,3 +80,89 @@ def test_rows_that_do_not_fit_leave_the_sequences_as_they_were(cache):
         with pytest.raises(ValueError):
             call()
         assert before == (cache.length, cache.free)
+
+
+@pytest.fixture
+def attention(cache):
+    """Two query heads for each of two key heads of 64 elements, rows of 32, positions up to 40."""
+    cache.view = type("View", (), dict(heads=2, dim=64))
+    cos = torch.zeros(40, 32)
+    return G.CachedAttention(cache, 4, torch.zeros((4 + 4) * 64, 32), torch.zeros(32, 4 * 64), cos, cos)
+
+
+def state(cache):
+    return dict(cache.length), {s: list(p) for s, p in cache.pages_of.items()}, list(cache.free)
+
+
+@pytest.mark.parametrize("rows", [lambda n: torch.zeros(n, 31), lambda n: torch.zeros(n, 32, dtype=torch.float64), lambda n: torch.zeros(n, 32, dtype=torch.bfloat16),
+                                  lambda n: torch.zeros(n, 32, 1), lambda n: torch.zeros(n, 32, device="meta")])
+def test_rows_of_another_kind_leave_the_sequences_as_they_were(attention, rows):
+    cache = attention.cache
+    cache.open("a"); cache.open("b")
+    cache.grow(["a", "b"], [15, 3])
+    before = state(cache)
+    for call in (lambda: attention.token(rows(2), ["a", "b"]), lambda: attention.prompt(rows(22), ["b", "a"], [20, 2])):
+        for _ in range(2):
+            with pytest.raises((ValueError, TypeError)):
+                call()
+            assert before == state(cache)
+
+
+@pytest.mark.parametrize("failing", ["moe_kv_cache_write", "moe_paged_attn_decode", "moe_kv_cache_read", "mm"])
+def test_a_step_that_fails_takes_its_growth_back(attention, monkeypatch, failing):
+    """Whatever raises after the pages have been handed out: lengths, pages and the order of the free ones are those before the step."""
+    cache = attention.cache
+
+    def fail(*_, **__):
+        raise MemoryError("no room")
+
+    monkeypatch.setattr(G.L, "moe_kv_cache_write", lambda view, k, v, slots, q, *_, **__: q)
+    monkeypatch.setattr(G.L, "moe_paged_attn_decode", lambda q, *_, **__: (q.contiguous(), None))
+    monkeypatch.setattr(G.L, "moe_kv_cache_read", lambda *_, rows, **__: (torch.zeros(rows, 2, 64), torch.zeros(rows, 2, 64)))
+    cache.open("a"); cache.open("b")
+    cache.grow(["a", "b"], [15, 3])
+    before = state(cache)
+    good = (lambda: attention.token(torch.zeros(2, 32), ["b", "a"]), lambda: attention.prompt(torch.zeros(35, 32), ["b", "a"], [18, 17]))
+    with monkeypatch.context() as broken:
+        broken.setattr(*((G.torch, "mm") if failing == "mm" else (G.L, failing)), fail)
+        for call in good[:1] if failing == "moe_paged_attn_decode" else good[1:] if failing == "moe_kv_cache_read" else good:
+            with pytest.raises(MemoryError):
+                call()
+            assert before == state(cache)
+    # the last projection alone
+    mm = torch.mm
+    with monkeypatch.context() as broken:
+        broken.setattr(G.torch, "mm", lambda x, w: fail() if w.shape[1] == 32 else mm(x, w))
+        for call in good:
+            with pytest.raises(MemoryError):
+                call()
+            assert before == state(cache)
+    assert good[0]().shape == (2, 32) and cache.length == {"a": 16, "b": 4}
+    assert good[1]().shape == (35, 32) and cache.length == {"a": 33, "b": 22}
+
+
+def test_growth_is_taken_back_where_its_tables_cannot_be_made(cache, monkeypatch):
+    cache.open("a")
+    before = state(cache)
+    with monkeypatch.context() as broken:
+        broken.setattr(G.torch, "tensor", lambda *_, **__: (_ for _ in ()).throw(RuntimeError("no room")))
+        with pytest.raises(RuntimeError):
+            cache.grow(["a"], [40])
+    assert before == state(cache)
+
+
+def test_shrink_undoes_grow(cache):
+    cache.open("a"); cache.open("b")
+    cache.grow(["a", "b"], [17, 1])
+    for seqs, counts in ((["a", "b"], [15, 15]), (["b", "a"], [20, 30]), (["a"], [0]), (["b"], [31])):
+        before = state(cache)
+        cache.grow(seqs, counts)
+        cache.shrink(seqs, counts)
+        assert before == state(cache)
+    cache.shrink(["a"], [17])
+    assert cache.length["a"] == 0 and cache.pages_of["a"] == [] and len(cache.free) == 5
+    for bad in (["b", "b"], [1, 1]), (["b"], [2]), (["b"], [-1]), (["b"], []):
+        before = state(cache)
+        with pytest.raises(ValueError):
+            cache.shrink(*bad)
+        assert before == state(cache)
