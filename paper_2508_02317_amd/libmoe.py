@@ -589,22 +589,33 @@ class KVCacheView:
         self.heads, self.dim, self.page_size, self.scale = heads, dim, page_size, dim ** -0.5
         self.desc = moe_kv_cache_t(code, pages, heads, page_size, dim, 0, _ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), k.stride(0),
                                    k_scales.stride(0) if code == MOE_MX8 else 0)
-        self.ref = ctypes.addressof(self.desc)
+        self._ref = ctypes.addressof(self.desc)
+        self._at = tuple((name, getattr(self, name).data_ptr()) for name in ("k", "v", "k_scales", "v_scales")[:4 if code == MOE_MX8 else 2])
+
+    @property
+    def ref(self):
+        """The descriptor's address, for a call.  It holds the tensors' addresses: one whose storage has been swapped, resized or freed since may
+        not be reached through it any more."""
+        for name, at in self._at:
+            if getattr(self, name).data_ptr() != at:
+                raise ValueError("%s of the cache has moved since its view was made" % name)
+        return self._ref
 
 
 def moe_kv_cache(k, v, k_scales=None, v_scales=None):
     """k, v [pages, heads, page_size, dim] f32, bf16, or uint8 codes with scales uint8 [pages, heads, page_size, dim / 32].
-    -> the view of them that moe_kv_cache_write, moe_kv_cache_read and moe_paged_attn_decode take (it keeps the tensors)."""
+    -> the view of them that moe_kv_cache_write, moe_kv_cache_read and moe_paged_attn_decode take (it keeps the tensors, which stay where they are)."""
     return KVCacheView(k, v, k_scales, v_scales)
 
 
 def moe_kv_cache_write(cache, k, v, slots, q=None, positions=None, cos=None, sin=None, interleaved=False, q_out=None):
     """k, v [T, heads, dim] into the cache at slots [T] i64, the keys rotated if a table is given; q [T, Hq, dim] rotated into q_out.
     -> q_out (None without q)."""
+    ref = cache.ref
     if q is not None and q_out is None:
         q_out = torch.empty(q.shape, dtype=cache.dtype, device=q.device)
     if _marshal is not None:
-        _check(_marshal.kv_cache_write(cache.ref, k, v, slots, q, positions, cos, sin, interleaved, q_out, _stream()))
+        _check(_marshal.kv_cache_write(ref, k, v, slots, q, positions, cos, sin, interleaved, q_out, _stream()))
         return q_out
     T, dt = k.shape[0], cache.dtype
     shape = (T, cache.heads, cache.dim)
@@ -618,7 +629,7 @@ def moe_kv_cache_write(cache, k, v, slots, q=None, positions=None, cos=None, sin
         Hq = q.shape[1]
         qi, qo = _heads(q, dt, "q", (T, Hq, cache.dim)), _heads(q_out, dt, "q_out", q.shape)
     p_pos, p_cos, p_sin, n_pos, rot = _table(cos, sin, positions, T)
-    _check(lib.moe_kv_cache_write(cache.ref, *ki, *vi, T, slots.data_ptr(), *qi, Hq, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, _stream()))
+    _check(lib.moe_kv_cache_write(ref, *ki, *vi, T, slots.data_ptr(), *qi, Hq, rot, p_pos, p_cos, p_sin, n_pos, interleaved, *qo, _stream()))
     return q_out
 
 
@@ -626,13 +637,14 @@ def moe_kv_cache_read(cache, pages, row_start, rows=None, first=None, out=None):
     """Tokens first[b] .. of every sequence b (first None: from its first on) into the rows row_start[b] .. row_start[b + 1] - 1.
     pages [B, max_pages] i32, row_start [B + 1] i32, first [B] i32; rows: row_start[B], needed without out.
     -> k, v [rows, heads, dim] in the cache's type (bf16 for 8-bit codes)."""
+    ref = cache.ref
     if out is None:
         if rows is None:
             raise ValueError("rows (the last of row_start, on the host) or out must be given")
         out = tuple(torch.empty((rows, cache.heads, cache.dim), dtype=cache.dtype, device=pages.device) for _ in range(2))
     k, v = out
     if _marshal is not None:
-        _check(_marshal.kv_cache_read(cache.ref, pages, row_start, first, k, v, _stream()))
+        _check(_marshal.kv_cache_read(ref, pages, row_start, first, k, v, _stream()))
         return out
     _need(pages, torch.int32, "pages"); _need(row_start, torch.int32, "row_start")
     if pages.dim() != 2 or row_start.numel() != pages.shape[0] + 1:
@@ -645,7 +657,7 @@ def moe_kv_cache_read(cache, pages, row_start, rows=None, first=None, out=None):
     _need(k, cache.dtype, "k out"); _need(v, cache.dtype, "v out")
     if k.dim() != 3 or k.shape[1:] != (cache.heads, cache.dim) or v.shape != k.shape:
         raise ValueError("out must be two tensors [rows, %d, %d]" % (cache.heads, cache.dim))
-    _check(lib.moe_kv_cache_read(cache.ref, pages.data_ptr(), max_pages, row_start.data_ptr(), _ptr(first), B, k.shape[0], k.data_ptr(), v.data_ptr(),
+    _check(lib.moe_kv_cache_read(ref, pages.data_ptr(), max_pages, row_start.data_ptr(), _ptr(first), B, k.shape[0], k.data_ptr(), v.data_ptr(),
                                  _stream()))
     return out
 
@@ -653,6 +665,7 @@ def moe_kv_cache_read(cache, pages, row_start, rows=None, first=None, out=None):
 def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None, lse=None, ws=None):
     """Attention of one token per sequence: q [B, Hq, dim] over the first lens[b] tokens of the pages pages[b, :] (the last `window` of them
     where it is not 0).  scale None: dim ** -0.5.  -> out [B, Hq, dim], lse [B, Hq] f32 (None where lse is not given; True makes one)."""
+    ref = cache.ref
     if scale is None:
         scale = cache.scale
     if out is None:
@@ -663,7 +676,7 @@ def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None,
         B, Hq, _ = q.shape
         ws, _ = _ws(lib.moe_paged_attn_decode_workspace_bytes, (B, Hq, cache.heads, cache.dim, cache.page_size, pages.shape[1]), None, q.device)
     if _marshal is not None:
-        _check(_marshal.paged_attn_decode(cache.ref, q, pages, lens, scale, window, out, lse, ws, _stream()))
+        _check(_marshal.paged_attn_decode(ref, q, pages, lens, scale, window, out, lse, ws, _stream()))
         return out, lse
     dt = cache.dtype
     B, Hq, _ = q.shape
@@ -677,6 +690,6 @@ def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None,
         raise ValueError("lse must be [%d, %d]" % (B, Hq))
     if window != ctypes.c_int32(window).value:
         raise OverflowError("window does not fit 32 bits")
-    _check(lib.moe_paged_attn_decode(*qi, cache.ref, pages.data_ptr(), pages.shape[1], lens.data_ptr(), B, Hq, scale, window, out.data_ptr(), _ptr(lse),
+    _check(lib.moe_paged_attn_decode(*qi, ref, pages.data_ptr(), pages.shape[1], lens.data_ptr(), B, Hq, scale, window, out.data_ptr(), _ptr(lse),
                                      ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
     return out, lse

@@ -115,3 +115,39 @@ def test_the_binding_refuses_what_is_not_a_cache(L):
         L.moe_kv_cache(mk(2, 2, 16, 128), mk(2, 2, 16, 128))         # not on a device
     with pytest.raises(TypeError):
         L.moe_kv_cache(mk(2, 2, 16, 128, t=torch.float16), mk(2, 2, 16, 128))
+
+
+@pytest.mark.parametrize("which", ["k", "v", "k_scales", "v_scales"])
+@pytest.mark.parametrize("how", ["swapped", "grown", "emptied", "replaced"])
+def test_a_view_whose_tensor_has_moved_is_refused(L, which, how):
+    """Calls go to the memory that the view's tensors had when it was made; where one has other memory by now, they are refused."""
+    import torch
+
+    class OnDevice(torch.Tensor):                                    # memory of the host that says it is a device's: nothing is launched
+        is_cuda = True
+
+    mk = lambda *s: torch.zeros(s, dtype=torch.uint8).as_subclass(OnDevice)
+    view = L.moe_kv_cache(mk(3, 1, 16, 64), mk(3, 1, 16, 64), mk(3, 1, 16, 2), mk(3, 1, 16, 2))
+    k, pages, lens = torch.zeros(2, 1, 64, dtype=torch.bfloat16), torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    out = (torch.zeros(2, 1, 64, dtype=torch.bfloat16),) * 2
+    calls = (lambda: L.moe_kv_cache_write(view, k, k, lens.long()), lambda: L.moe_kv_cache_read(view, pages, lens, out=out),
+             lambda: L.moe_paged_attn_decode(k, view, pages, lens, out=out[0], ws=torch.zeros(4096)))
+    assert view.ref == ctypes.addressof(view.desc)
+    for call in calls:
+        with pytest.raises(Exception) as e:                          # these are not on a device, and are refused for that
+            call()
+        assert "moved" not in str(e.value)
+    t = getattr(view, which)
+    was = t.data_ptr()
+    if how == "swapped":
+        t.data = torch.ones_like(t)
+    elif how == "grown":
+        t.resize_(3 << 20)
+    elif how == "emptied":
+        t.untyped_storage().resize_(0)
+    else:
+        setattr(view, which, mk(*t.shape))
+    assert getattr(view, which).data_ptr() != was
+    for call in calls:
+        with pytest.raises(ValueError, match="%s.* moved" % which):
+            call()
