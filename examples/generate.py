@@ -34,11 +34,15 @@ class Block:
         self._layers = {}
 
     def moe(self, x):
-        """The MoE layer for this number of rows (its buffers are made once per size)."""
-        layer = self._layers.get(len(x))
+        """The MoE layer for this number of rows.  Its buffers are large (gradients of the weights among them), so that of the last two sizes are kept: a
+        prompt's and a step's."""
+        layer = self._layers.pop(len(x), None)
+        while len(self._layers) > 1:
+            del self._layers[next(iter(self._layers))]               # the one used longest ago, before another is made
         if layer is None:
-            layer = self._layers[len(x)] = MoELayer(len(x), self.d, self.experts, self.k, self.f, torch.bfloat16, self.w_gate, self.w_up, self.w_down,
-                                                    w_router=self.w_router, gather=True, save_gu=False)
+            layer = MoELayer(len(x), self.d, self.experts, self.k, self.f, torch.bfloat16, self.w_gate, self.w_up, self.w_down, w_router=self.w_router, gather=True,
+                             save_gu=False)
+        self._layers[len(x)] = layer
         return layer.forward(x)
 
     @staticmethod

@@ -166,3 +166,34 @@ def test_shrink_undoes_grow(cache):
         with pytest.raises(ValueError):
             cache.shrink(*bad)
         assert before == state(cache)
+
+
+def test_the_example_keeps_a_bounded_number_of_layers(monkeypatch):
+    """A layer's buffers go with its number of rows and are large; prompts come in any number of rows."""
+    import os
+    import sys
+    import weakref
+    monkeypatch.syspath_prepend(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import generate
+    made = []
+
+    class Layer:
+        def __init__(self, rows, *_, **__):
+            self.rows = rows
+            made.append(weakref.ref(self))
+
+        def forward(self, x):
+            assert len(x) == self.rows
+            return x
+
+    monkeypatch.setattr(generate, "MoELayer", Layer)
+    block = object.__new__(generate.Block)
+    block.d = block.experts = block.k = block.f = 1
+    block.w_gate = block.w_up = block.w_down = block.w_router = None
+    block._layers = {}
+    for prompt in range(20, 40):
+        for rows in (prompt, 4, 4, 4):
+            assert len(block.moe(torch.zeros(rows, 1))) == rows
+            assert sum(ref() is not None for ref in made) <= 2
+    assert len(made) == 20 + 1                                       # the one of the steps is kept over the prompts
+    sys.modules.pop("generate")
