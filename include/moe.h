@@ -320,7 +320,8 @@ int32_t moe_rope_bwd(const void* dq, int64_t q_stride_t, int64_t q_stride_h, con
  * Paged key/value cache for generation (a widening beyond the paper, which trains).
  * A page holds page_size consecutive tokens of one sequence, for all key/value heads:
  *   k, v [pages, heads, page_size, dim] of dtype MOE_F32 or MOE_BF16, or MOE_MX8: E4M3 codes (one byte an element) with
- *   k_scales, v_scales [pages, heads, page_size, dim/32] u8, value = 2^(scale - 127) * code, blocks and rounding as in moe_mx8_quantise.
+ *   k_scales, v_scales [pages, heads, page_size, dim/32] u8, value = 2^(scale - 127) * code, blocks and rounding as in moe_mx8_quantise;
+ *   a scale of 255 makes its block NaN.
  *   page_stride, scale_page_stride: elements (bytes for the scales) from one page to the next; within a page all is dense.
  *   page_size a power of two from 16 to 4096; dim 64, 128, 192 or 256.
  * The descriptor is read on the host during a call [host]; its pointers are device pointers.

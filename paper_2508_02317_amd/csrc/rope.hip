@@ -291,8 +291,8 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
         if (h + u >= h1) break;
         const bool is_v = h + u >= H;
         if constexpr (KIND == MOE_MX8) {
-          // 2^(s - 127); s = 0 is the subnormal 2^-127.  A code times it fits bf16 whole unless it falls below bf16's smallest numbers.
-          const float sc = scale[u] != 0u ? __uint_as_float(scale[u] << 23) : __uint_as_float(0x00400000u);
+          // 2^(s - 127); s = 0 is the subnormal 2^-127, s = 255 NaN.  A code times it fits bf16 whole unless it falls below bf16's smallest numbers.
+          const float sc = __uint_as_float(scale[u] == 0u ? 0x00400000u : scale[u] == 255u ? 0x7FC00000u : scale[u] << 23);
           float v[8];
 #pragma unroll
           for (int q = 0; q < 2; ++q) {

@@ -200,3 +200,26 @@ def test_cache_beyond_32_bits():
     a = L.moe_paged_attn_decode(q, cache, table, lens, window=20)
     b = L.moe_paged_attn_decode(q, small, table - (pages - 3), lens, window=20)
     assert torch.equal(a[0], b[0])
+
+
+@pytest.mark.parametrize("D", [64, 128, 192])
+def test_a_scale_of_255_is_not_a_number_to_every_reader(D):
+    """Its block reads as NaN whatever the codes, in the copy and in the attention alike, and no other element does."""
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    cache = make_cache("mx8", 3, 2, 16, D)
+    cache.k_scales.fill_(127); cache.v_scales.fill_(127)
+    cache.k.copy_(torch.arange(cache.k.numel(), device="cuda").remainder(0x7F).to(torch.uint8).view(cache.k.shape))
+    table = to_dev(np.array([[2, 0]], dtype=np.int32))
+    start, lens = to_dev(np.array([0, 20], dtype=np.int32)), to_dev(np.array([20], dtype=np.int32))
+    q = torch.randn((1, 2, D), device="cuda").bfloat16()
+    whole, (att, _) = L.moe_kv_cache_read(cache, table, start, rows=20), L.moe_paged_attn_decode(q, cache, table, lens)
+    cache.k_scales[0, 1, 2, 1] = 255                                 # token 18, second head, elements 32 .. 63
+    cache.v_scales[2, 0, 5, 0] = 255                                 # token 5, first head, elements 0 .. 31
+    got, (out, lse) = L.moe_kv_cache_read(cache, table, start, rows=20), L.moe_paged_attn_decode(q, cache, table, lens, lse=True)
+    for x, ref, (t, h, at) in zip(got, whole, ((18, 1, 32), (5, 0, 0))):
+        hit = torch.zeros_like(x, dtype=torch.bool)
+        hit[t, h, at:at + 32] = True
+        assert torch.isnan(x[hit]).all() and torch.equal(x[~hit], ref[~hit])
+    assert torch.isnan(out[0, 1]).all() and torch.isnan(lse[0, 1]) and torch.isfinite(lse[0, 0])
+    assert torch.isnan(out[0, 0, :32]).all() and torch.equal(out[0, 0, 32:], att[0, 0, 32:])
