@@ -251,3 +251,100 @@ def test_infinite_and_not_a_number_values_where_they_count(kind, lens):
     hit = torch.zeros_like(out, dtype=torch.bool)
     hit[0, :2, 7] = hit[1, 2:, 60] = True
     assert torch.equal(lse, ref_lse) and not torch.isfinite(out[hit]).any() and torch.equal(out[~hit], ref[~hit])
+
+
+def run_on_a_used_workspace(kind, lens, Hq, H, D, ps, window=0, only=None):
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    say("attend %s %d sequences of up to %d Hq=%d H=%d D=%d page=%d window=%d, workspace of random bytes" % (kind, len(lens), max(lens), Hq, H, D, ps, window))
+    cache, q, table, n = build(kind, lens, Hq, H, D, ps, 11)
+    ws = torch.randint(0, 256, (L.lib.moe_paged_attn_decode_workspace_bytes(len(lens), Hq, H, D, ps, table.shape[1]),), device="cuda").to(torch.uint8)
+    out, lse = L.moe_paged_attn_decode(q, cache, to_dev(table), to_dev(n), window=window, lse=True, ws=ws)
+    verify(kind, cache, q, table, n, out, lse, ps, D ** -0.5, window, only)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mx8"])
+@pytest.mark.parametrize("window", [1000, 1017])
+@pytest.mark.parametrize("Hq,H,D", [(8, 2, 128), (34, 2, 64), (4, 1, 256)])
+def test_windows_that_are_cut_into_pieces(kind, window, Hq, H, D):
+    """Windows of 32 stretches and more, which begin far behind the context's first tokens, on and off the multiples of a stretch and a page."""
+    run_on_a_used_workspace(kind, [5000, 1700, 0, 1001, 3], Hq, H, D, 16 if D == 64 else 32, window)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mx8"])
+@pytest.mark.parametrize("window", [0, 1003])
+def test_more_than_256_sequences_of_which_some_are_cut(kind, window):
+    r = np.random.default_rng(12)
+    lens = [int(x) for x in r.integers(0, 40, 300)]
+    for b, n in ((0, 2100), (129, 1500), (251, 3000), (255, 0), (259, 1999), (299, 1501)):
+        lens[b] = n
+    lens[230:250], lens[254:259] = [0] * 20, [0] * 5
+    run_on_a_used_workspace(kind, lens, 4, 2, 64, 16, window, only=[0, 1, 128, 129, 130, 229, 230, 249, 250, 251, 252, 253, 254, 255, 256, 257, 258, 259, 260, 298, 299])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mx8"])
+@pytest.mark.parametrize("longest", [600, 1000, 1100])
+def test_many_units_around_the_length_from_which_contexts_are_cut(kind, longest):
+    """256 units: 32 stretches (1024 tokens, half in fp32 heads of 128) are one piece each, more are cut."""
+    r = np.random.default_rng(13)
+    lens = [int(x) for x in r.integers(1, longest, 128)]
+    lens[5], lens[60], lens[127] = longest, 0, longest - 1
+    run_on_a_used_workspace(kind, lens, 4, 2, 128, 16, only=[0, 5, 6, 59, 60, 61, 126, 127])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[400, 90], [3000, 70]])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_a_poisoned_key_leaves_the_other_heads_their_bits(kind, lens, bad):
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    cache, q, table, n = build(kind, lens, 4, 2, 64, 16, 14)
+    q[..., 0] = 1.0
+    dev = to_dev(table), to_dev(n)
+    ref, ref_lse = L.moe_paged_attn_decode(q, cache, *dev, lse=True)
+    cache.k[int(table[0, 1]), 0, 2, 0] = float(bad)                  # the first context's token 18: heads 0 and 1
+    cache.k[int(table[1, 4]), 1, 3, 0] = float(bad)                  # the second's token 67: heads 2 and 3
+    out, lse = L.moe_paged_attn_decode(q, cache, *dev, lse=True)
+    hit = torch.zeros((2, 4), dtype=torch.bool, device="cuda")
+    hit[0, :2] = hit[1, 2:] = True
+    assert torch.isnan(out[hit]).all() and not torch.isfinite(lse[hit]).any()
+    assert torch.equal(out[~hit], ref[~hit]) and torch.equal(lse[~hit], ref_lse[~hit])
+
+
+@pytest.mark.parametrize("k_code,v_code,q_power", [(0, 127, 120), (1, 127, 120), (254, 127, -120), (127, 240, 0)])
+def test_scales_at_the_ends_of_their_range(k_code, v_code, q_power):
+    """Keys' scales from 2^-127 to 2^127, with queries and a scale that bring the scores back; large ones of values.  Elements from 2 on where scales are the
+    smallest (nothing below bf16's normal numbers), up to 1 where they are the largest (no sum beyond fp32's range)."""
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    cache, q, table, n = build("mx8", [91, 700], 8, 2, 128, 16, 15)
+    for t, s, code in ((cache.k, cache.k_scales, k_code), (cache.v, cache.v_scales, v_code)):
+        sign, size = t & 0x80, t & 0x7F
+        size = torch.where(size == 0x7F, size, size.clamp(min=0x40) if code < 8 else size.clamp(max=0x38) if code > 200 else size)     # 0x7F: places of nobody
+        t.copy_(sign | size)
+        s.copy_(torch.where(s == 255, s, code))
+    q = (q.double() * 2.0 ** q_power).bfloat16()
+    scale = float(np.float32(0.01 * 2.0 ** (127 - k_code - q_power)))
+    out, lse = L.moe_paged_attn_decode(q, cache, to_dev(table), to_dev(n), scale=scale, lse=True)
+    verify("mx8", cache, q, table, n, out, lse, 16, scale)
+
+
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+def test_the_value_of_a_single_token_comes_out_as_it_is(D):
+    """Every code with every scale, down to bf16's smallest numbers: p is 1, so the output is the value, as the cache's reader has it."""
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    scales, codes = torch.arange(255, device="cuda").to(torch.uint8), torch.arange(256, device="cuda").to(torch.uint8)
+    codes[(codes & 0x7F) == 0x7F] = 0x5A                             # but NaN
+    for part in codes.split(D) if 256 % D == 0 else (codes[:D], codes[-D:]):
+        cache = make_cache("mx8", 255, 1, 16, D)
+        cache.v[:, 0, 0] = part
+        cache.v_scales[:, 0, 0] = scales[:, None]
+        table, lens = torch.arange(255, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.ones(255, dtype=torch.int32, device="cuda")
+        out, _ = L.moe_paged_attn_decode(torch.ones((255, 3, D), dtype=torch.bfloat16, device="cuda"), cache, table, lens)
+        _, v = L.moe_kv_cache_read(cache, table, torch.arange(256, dtype=torch.int32, device="cuda"), rows=255)
+        ref = A.F.e4m3_decode(to_np(part)) * np.exp2(np.arange(255.0) - 127)[:, None]
+        normal = (np.abs(ref) >= 2.0 ** -126) & (np.abs(ref) < 2.0 ** 128)
+        assert np.array_equal(to_np(v)[:, 0][normal], ref[normal])
+        there = torch.isfinite(v).expand_as(out)
+        assert torch.equal(out[there], v.expand_as(out)[there]) and not torch.isfinite(out[~there]).any()

@@ -183,3 +183,33 @@ def test_steps_of_no_sequences_and_chunks_of_no_tokens():
     y = block.attention.prompt(x, [0, 1], [0, 21])                   # one of them has something to say
     block.cache.open(2)
     assert torch.equal(y, block.attention.prompt(x, [2], [21])) and block.cache.length == {0: 0, 1: 21, 2: 21}
+
+
+@pytest.mark.parametrize("eight_bit", [False, True])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("window", [0, 12])
+def test_prompts_and_steps_of_sharp_heads_element_by_element(eight_bit, interleaved, window):
+    """Both ways through the layer, the attention alone: keys, values and queries are known bit for bit, so every element has the tolerance of one attention."""
+    import torch
+    from paper_2508_02317_amd.generation import CachedAttention, PagedKVCache
+    from tests import attn_step as S
+    from tests.util import to_dev
+    rows, w, w_out, cos, sin = S.inputs(22)
+    attention = CachedAttention(PagedKVCache(40, 16, S.KV_HEADS, S.DIM, eight_bit=eight_bit), S.HEADS, to_dev(w, "bf16"), to_dev(w_out, "bf16"), to_dev(cos), to_dev(sin),
+                                interleaved, window)
+    seqs = list(range(len(rows)))
+    for s in seqs:
+        attention.cache.open(s)
+    y = to_np(attention.prompt(to_dev(np.concatenate([x[:n] for x, n in zip(rows, S.LENGTHS)]), "bf16"), seqs, list(S.LENGTHS)))
+    got = [list(part) for part in np.split(y, np.cumsum(S.LENGTHS)[:-1])]
+    for i in range(S.STEPS):
+        order = seqs[i % 4:] + seqs[:i % 4]                          # in any order
+        y = to_np(attention.token(to_dev(np.stack([rows[s][S.LENGTHS[s] + i] for s in order]), "bf16"), order))
+        for s, row in zip(order, y):
+            got[s].append(row)
+    for x, out in zip(rows, got):
+        q, k, v = S.projected(x, w, cos, sin, interleaved, eight_bit)
+        for t, row in enumerate(out):
+            ref, tol = S.expected(q, k, v, t, window)
+            bad = ~(np.abs(row.reshape(S.HEADS, S.DIM).astype(np.float64) - ref) <= tol)
+            assert not bad.any(), "token %d of %d: %d elements off, worst by %.3g of the bound" % (t, len(x), bad.sum(), (np.abs(row.reshape(ref.shape) - ref) / tol).max())

@@ -223,3 +223,21 @@ def test_a_scale_of_255_is_not_a_number_to_every_reader(D):
         assert torch.isnan(x[hit]).all() and torch.equal(x[~hit], ref[~hit])
     assert torch.isnan(out[0, 1]).all() and torch.isnan(lse[0, 1]) and torch.isfinite(lse[0, 0])
     assert torch.isnan(out[0, 0, :32]).all() and torch.equal(out[0, 0, 32:], att[0, 0, 32:])
+
+
+@pytest.mark.parametrize("kind,T,Hq,H,D,rot,ps,interleaved", CASES)
+def test_a_store_without_queries_or_a_rotation_leaves_keys_and_values_as_they_are(kind, T, Hq, H, D, rot, ps, interleaved):
+    """All four tensors of the cache, everything that was not stored into among them."""
+    from paper_2508_02317_amd import libmoe as L
+    say("kv write alone %s T=%d H=%d D=%d page=%d" % (kind, T, H, D, ps))
+    r = np.random.default_rng(T + D)
+    k, v = (to_dev((r.standard_normal((T, H, D)) * np.exp(r.uniform(-3, 3, (T, 1, 1)))).astype(np.float32), "f32" if kind == "f32" else "bf16") for _ in range(2))
+    pages = T // ps + 2
+    slots = r.permutation(pages * ps)[:T].astype(np.int64)
+    cache = make_cache(kind, pages, H, ps, D)
+    want = snapshot(cache)
+    L.moe_kv_cache_write(cache, k, v, to_dev(slots))
+    store(want[0], kind, to_np(k), want[2], slots, ps)
+    store(want[1], kind, to_np(v), want[3], slots, ps)
+    for got, ref, name in zip(snapshot(cache), want, ("k", "v", "k_scales", "v_scales")):
+        assert ref is None or np.array_equal(got, ref), name
