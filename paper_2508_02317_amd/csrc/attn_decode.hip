@@ -42,6 +42,7 @@
 #include "attn_plan.h"
 #include "launch_plan.h"
 #include "moe_common.h"
+#include "mx8_codes.h"
 
 namespace moe {
 
@@ -87,9 +88,6 @@ __device__ __forceinline__ float row_sum4(float v) {
   v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-__device__ __forceinline__ float scale_of(uint32_t code) {   // 2^(code - 127)
-  return __uint_as_float(code << 23);
 }
 // 16 rows of a page as a buffer: a lane's offset is the same for all tokens, and rows that are not there (range 0) are not fetched, so that loads
 // ahead need no branch around them.
@@ -213,7 +211,7 @@ template <int KIND, int D> struct Wave {
           for (int j = 0; j < 4; ++j)
             t[a][j % kChains] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[a][i][j]), __uint_as_float(q[i][j]), t[a][j % kChains], 0, 0, 0);
         } else if constexpr (kMx) {
-          const float sc = scale_of((ks[a].pair(i) >> (8 * (c >> 1))) & 0xFFu);
+          const float sc = mx_scale((ks[a].pair(i) >> (8 * (c >> 1))) & 0xFFu);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
             t[a][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(k[a][i][2 * h], k[a][i][2 * h + 1], sc), __builtin_bit_cast(bf16x8, q[2 * i + h]), t[a][0], 0, 0, 0);
@@ -310,7 +308,7 @@ template <int KIND, int D> struct Wave {
           const int vt = 4 * two + t;
           if constexpr (kMx) {
             const int at = (t & 3) * kScaleRow + g * (kG / 32);        // byte of the first of the row's scales for this group
-            const float sc = scale_of((vs[vt >> 2][at >> 2] >> (8 * ((at & 3) + n * kE / 32))) & 0xFFu);
+            const float sc = mx_scale((vs[vt >> 2][at >> 2] >> (8 * ((at & 3) + n * kE / 32))) & 0xFFu);
 #pragma unroll
             for (int e = 0; e < kE / 4; ++e) {
               w[t][2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[vt][g][e], sc, false));

@@ -22,6 +22,8 @@ __device__ __forceinline__ uint32_t mx_scale_code(float amax) {
 }
 // 1 / scale = 2^(127 - code), exact
 __device__ __forceinline__ float mx_inverse_scale(uint32_t code) { return __builtin_bit_cast(float, (254u - code) << 23); }
+// 2^(code - 127) for the scaled conversions, which look at its exponent alone: 0 stands for 2^-127, 255 for NaN
+__device__ __forceinline__ float mx_scale(uint32_t code) { return __builtin_bit_cast(float, code << 23); }
 // eight values -> eight E4M3 codes (the hardware conversion rounds to nearest even; it does not saturate)
 __device__ __forceinline__ uint2 mx_encode8(const float (&v)[8], float inv) {
   float s[8];

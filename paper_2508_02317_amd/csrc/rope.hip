@@ -291,15 +291,13 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheReadArgs a, i
         if (h + u >= h1) break;
         const bool is_v = h + u >= H;
         if constexpr (KIND == MOE_MX8) {
-          // 2^(s - 127); s = 0 is the subnormal 2^-127, s = 255 NaN.  A code times it fits bf16 whole unless it falls below bf16's smallest numbers.
-          const float sc = __uint_as_float(scale[u] == 0u ? 0x00400000u : scale[u] == 255u ? 0x7FC00000u : scale[u] << 23);
-          float v[8];
+          // exact in bf16 down to its smallest numbers
+          const float sc = mx_scale(scale[u]);
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
-            const f32x2 l = __builtin_amdgcn_cvt_pk_f32_fp8(code[u][q], false), m = __builtin_amdgcn_cvt_pk_f32_fp8(code[u][q], true);
-            v[4 * q] = l[0] * sc; v[4 * q + 1] = l[1] * sc; v[4 * q + 2] = m[0] * sc; v[4 * q + 3] = m[1] * sc;
+            x[u].w[2 * q] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[u][q], sc, false));
+            x[u].w[2 * q + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code[u][q], sc, true));
           }
-          x[u].set(v);
         }
         E* dst = static_cast<E*>(is_v ? a.v_out : a.k_out);
         x[u].store(dst + (r * H + (is_v ? h + u - H : h + u)) * D + chunk * N);
