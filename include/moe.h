@@ -363,8 +363,10 @@ int32_t moe_kv_cache_read(const moe_kv_cache_t* cache, const int32_t* block_tabl
  *   A sequence without tokens gets zeros and lse = -inf.  Places of the cache outside a sequence's tokens may hold anything.
  *   A value of theirs that is infinite or NaN makes the same element of its heads' outputs infinite or NaN, and no other.
  *   Scores, softmax and sums are fp32; the result is rounded once.  Page ids are taken as the nearest that exists.
+ *   The sum of exp(score - greatest score) |v_t| has to stay within fp32's range: it is divided by the weights' sum at the end.
  *   The order of the sums depends on lens, B and the sizes only: the same call gives the same bits.
- *   Hq a multiple of heads; B * heads * context length up to 2^31 or so (MOE_ERR_UNSUPPORTED beyond).
+ *   Hq a multiple of heads; page tables for contexts below 2^31 tokens, B * Hq up to 2^23, and B * heads * the tokens of a row of the page table (or of
+ *   the window) below 2^36, 2^35 for f32 heads of more than 64 elements, less by the number of units of 16 query heads per head (MOE_ERR_UNSUPPORTED beyond).
  */
 size_t moe_paged_attn_decode_workspace_bytes(int B, int Hq, int heads, int dim, int page_size, int max_pages);
 int32_t moe_paged_attn_decode(const void* q, int64_t q_stride_b, int64_t q_stride_h, const moe_kv_cache_t* cache,

@@ -2,8 +2,8 @@
 //
 //     out[b, h] = sum_t p_t v_t / sum_t p_t,   p_t = exp(scale <q[b, h], k_t> - m),   m = max_t scale <q[b, h], k_t>
 //
-// All heads of a group share their keys and values, so an element of the cache is read once and used for the whole group: 2 * 16 operations
-// per byte at most (bf16, 16 heads), far below what the matrix units need to be busy.  The kernel is bound by the rate at which the cache
+// All heads of a group share their keys and values, so an element of the cache is read once and used for the whole group: 16 operations
+// per byte at most (bf16, 16 heads; 31 in 8 bits), far below what the matrix units need to be busy.  The kernel is bound by the rate at which the cache
 // arrives, and its layout serves that rate:
 //
 //   * No key or value passes through LDS.  A wave takes kSub tokens at a time, and the operands of the matrix instructions are what its lanes
@@ -25,7 +25,7 @@
 //     differ as they like.  A workgroup that does not see the whole context of a head leaves its maximum, sum and unscaled output behind, at most
 //     two of them, and a second launch joins those.  The cut depends on lens alone, so results do not change from call to call.  Tiles of kSub tokens
 //     would cut more evenly but leave three waves of four idle in a workgroup's last round: 16 contexts of up to 4096 tokens 24 -> 29.5 us.
-//     512 workgroups (256 of more than 128 elements) are what the card has room for; 768 and 1024 were 2 to 8 % slower.
+//     512 workgroups (256 for heads of more than 128 elements) are what the card has room for; 768 and 1024 were 2 to 8 % slower.
 //     Eight waves on half as many workgroups: 64 contexts of 8192 tokens 1 to 3 % faster, one of 100 to 1000 15 to 20 % slower.
 //
 // Scores are fp32 sums of exact products (8-bit values are exact in bf16).  p is split into two bf16 numbers, together exact to 2^-16, so that
@@ -660,9 +660,11 @@ Launch launch_of(int dtype, int dim, int B, int Hq, int Hkv, int page_size, int 
   l.heads = ceil_div(group, l.parts);
   const int64_t units = static_cast<int64_t>(B) * Hkv * l.parts, held = static_cast<int64_t>(page_size) * max_pages;
   const int64_t most_seen = static_cast<int64_t>(window) + l.sub, seen = window > 0 && most_seen < held ? most_seen : held, subs = (seen + l.sub - 1) / l.sub;   // a window may begin inside a stretch
-  // A context of few stretches is not cut (its one tile is the whole): a workgroup has it in a few turns, and no second launch is needed.
+  // Contexts of few stretches are not cut (a context's one tile is the whole): a workgroup has it in a few turns, and no second launch is needed.  The
+  // host does not have the lengths, so what the page table or the window has room for decides.
   // 4 key heads of 128 elements in bf16, cut -> whole: one context of 250 tokens 11.1 -> 7.9 us, 500 10.8 -> 9.5, 1000 10.8 -> 14.4; 64 contexts of
-  // 250 14.4 -> 10.2, 500 18.4 -> 14.6, 1000 27.2 -> 23.6; 512 of 250 63 -> 54, 1000 180 -> 173.
+  // 250 14.4 -> 10.2, 500 18.4 -> 14.6, 1000 27.2 -> 23.6; 512 of 250 63 -> 54, 1000 180 -> 173.  All of equal lengths: whole contexts are dealt out by
+  // their number, so ragged ones lose some of it (512 of up to 1000 tokens, 500 on average, 125 us; 512 of 500 95).
   l.cut = subs > (units >= 256 ? 32 : 16);
   l.tile_subs = l.cut ? kWaves : static_cast<int>(subs < 1 ? 1 : subs);
   l.most_subs = subs * units;

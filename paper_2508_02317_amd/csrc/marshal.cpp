@@ -1,6 +1,6 @@
 // Argument marshalling of the calls that a generation step makes many times: the checks of libmoe.py's functions on torch tensors and the call
 // into the C ABI, without the interpreter in between.  A small call is bound by the host: 256 tokens rotated take 4.5 us on the GPU
-// (launch to launch), 8.2 to be enqueued through ctypes and 4.3 from here.
+// (launch to launch), 9.1 to be enqueued through ctypes and 4.2 from here.
 // Built as a Python extension module beside libmoe_gfx950.so; libmoe.py uses it where it has been built.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>

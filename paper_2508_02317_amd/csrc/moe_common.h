@@ -91,7 +91,7 @@ __device__ __forceinline__ int wave_sum_i(int v) {
   return v;
 }
 
-// Integers that no launch of the call writes, the same for all lanes: read by scalar loads (a vector load among those of a stream of data
+// Integers that the kernel itself does not write, the same for all lanes: read by scalar loads (a vector load among those of a stream of data
 // would have to be waited for with them).
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 __device__ __forceinline__ ScalarInts scalar_ints(const int32_t* p) { return reinterpret_cast<ScalarInts>(reinterpret_cast<uintptr_t>(p)); }

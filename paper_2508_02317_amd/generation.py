@@ -5,7 +5,8 @@ transformer block over it.
     token    projection -> moe_kv_cache_write -> moe_paged_attn_decode -> projection
 
 The projections are plain library products; rotation, cache and the attention of single tokens are calls into libmoe on the current
-stream.  Which pages a sequence has is decided here, on the host, and reaches the device as one small copy per step.
+stream.  Which pages a sequence has is decided here, on the host, and reaches the device as four small tensors per step and layer, each
+a copy that the host waits for.
 """
 import math
 
@@ -51,7 +52,7 @@ def rope_amplitude(factor):
 class PagedKVCache:
     """Keys and values of one attention layer in pages of page_size tokens, and the pages of every sequence.
 
-    eight_bit: E4M3 codes with a power-of-two scale per 32 elements instead of bfloat16 (17/32 of the memory and of what attention reads)."""
+    eight_bit: E4M3 codes with a power-of-two scale per 32 elements instead of bfloat16 (33/64 of the memory and of what attention reads)."""
 
     def __init__(self, pages, page_size, heads, dim, dtype=torch.bfloat16, eight_bit=False, device="cuda"):
         if eight_bit and dtype is not torch.bfloat16:
