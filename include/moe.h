@@ -365,6 +365,7 @@ int32_t moe_kv_cache_read(const moe_kv_cache_t* cache, const int32_t* block_tabl
  *   Scores, softmax and sums are fp32; the result is rounded once.  Page ids are taken as the nearest that exists.
  *   The sum of exp(score - greatest score) |v_t| has to stay within fp32's range: it is divided by the weights' sum at the end.
  *   The order of the sums depends on lens, B and the sizes only: the same call gives the same bits.
+ *   lens is read in several places of the call: it must not be written, from another stream say, before the call has run.
  *   Hq a multiple of heads; page tables for contexts below 2^31 tokens, B * Hq up to 2^23, and B * heads * the tokens of a row of the page table (or of
  *   the window) below 2^36, 2^35 for f32 heads of more than 64 elements, less by the number of units of 16 query heads per head (MOE_ERR_UNSUPPORTED beyond).
  */
