@@ -316,6 +316,72 @@ int32_t moe_rope_bwd(const void* dq, int64_t q_stride_t, int64_t q_stride_h, con
                      const float* cos, const float* sin, int n_pos, int interleaved, void* dq_in, int64_t qo_stride_t,
                      int64_t qo_stride_h, void* dk_in, int64_t ko_stride_t, int64_t ko_stride_h, void* stream);
 
+/* The same with positions of several axes, as images and video have them (time, height, width): pair i of a head's elements turns by the position on
+ *   its axis pair_axis[i], i.e. c = cos[positions[pair_axis[i], t], i], s alike.  Everything else is as above.
+ *   positions [n_axes, T] i32, the positions of one axis after those of another; 1 <= n_axes <= 4.
+ *   pair_axis [rot/2] u8 [host], read during the call, every value below n_axes.
+ *   Axes with frequencies of their own are a matter of the table: column i belongs to pair i.
+ */
+int32_t moe_rope_axes_fwd(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k, int64_t k_stride_t,
+                          int64_t k_stride_h, int dtype, int T, int Hq, int Hk, int D, int rot, const int32_t* positions, int n_axes,
+                          const uint8_t* pair_axis, const float* cos, const float* sin, int n_pos, int interleaved, void* q_out,
+                          int64_t qo_stride_t, int64_t qo_stride_h, void* k_out, int64_t ko_stride_t, int64_t ko_stride_h, void* stream);
+int32_t moe_rope_axes_bwd(const void* dq, int64_t q_stride_t, int64_t q_stride_h, const void* dk, int64_t k_stride_t,
+                          int64_t k_stride_h, int dtype, int T, int Hq, int Hk, int D, int rot, const int32_t* positions, int n_axes,
+                          const uint8_t* pair_axis, const float* cos, const float* sin, int n_pos, int interleaved, void* dq_in,
+                          int64_t qo_stride_t, int64_t qo_stride_h, void* dk_in, int64_t ko_stride_t, int64_t ko_stride_h, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * The norm in front of each half of a block (RMSNorm and LayerNorm are among the efficient kernels of Sec. 3.2.5; the paper gives no formula).
+ *   h = x, or x + residual rounded to the element type (and stored in sum);  m = mean of a row of h, 0 when rms != 0;
+ *   r = 1 / sqrt(mean((h - m)^2) + eps);  y = (h - m) r weight + bias.  fp32 arithmetic, one rounding of y to the element type.
+ *   Rows are the D elements of a head: x [T, H, D], H = 1 for hidden states [T, D], with any strides (in elements) between tokens and heads that are multiples
+ *   of 16 bytes; the other tensors alike, each with its own strides.  residual and sum come together or are both NULL.
+ *   weight, bias [D] of type weight_dtype (MOE_F32, or MOE_BF16), or NULL: 1 and 0.
+ *   mean, rstd [T, H] f32 out, or NULL; mean is not written when rms != 0.
+ *   y may be x, and sum may be x or residual, with the same strides; other overlaps are not allowed.
+ * Backward of y with respect to h, for the upstream gradient dy:
+ *   g = dy weight,  xh = (h - m) r,  dx = r (g - mean(g) - xh mean(g xh)) + add   (without mean(g) for the rms norm);
+ *   dweight = sum over rows of dy xh,  dbias = sum over rows of dy, in fp32, rounded once to weight_dtype, overwritten.
+ *   x: what was normed (sum, where there was a residual).  mean, rstd [T, H] f32 as the forward call wrote them; mean == NULL means rms norm.
+ *   add [T, H, D] or NULL: the gradient that arrives at h by another way (the residual stream); dx is then the gradient of both x and residual.
+ *   dweight, dbias [D] or NULL (not wanted); ws is needed if one of them is.  dx may be dy, x or add, with the same strides.
+ * The order of all sums depends on the sizes only: the same call gives the same bits.  A NaN or an infinity in a row spoils that row of y and dx, and the sums
+ * over rows, and no other row.  The sum of a row's squares has to stay within fp32's range.
+ * D a multiple of 8 up to 16384, T * H within int32 (MOE_ERR_UNSUPPORTED beyond).  T == 0: nothing is read; dweight and dbias are written as zeros.
+ */
+int32_t moe_norm_fwd(const void* x, int64_t x_stride_t, int64_t x_stride_h, const void* residual, int64_t r_stride_t, int64_t r_stride_h,
+                     int dtype, int T, int H, int D, int rms, const void* weight, const void* bias, int weight_dtype, float eps,
+                     void* sum, int64_t s_stride_t, int64_t s_stride_h, void* y, int64_t y_stride_t, int64_t y_stride_h, float* mean,
+                     float* rstd, void* stream);
+size_t moe_norm_bwd_workspace_bytes(int T, int H, int D);
+int32_t moe_norm_bwd(const void* dy, int64_t dy_stride_t, int64_t dy_stride_h, const void* x, int64_t x_stride_t, int64_t x_stride_h,
+                     int dtype, int T, int H, int D, const float* mean, const float* rstd, const void* weight, int weight_dtype,
+                     const void* add, int64_t add_stride_t, int64_t add_stride_h, void* dx, int64_t dx_stride_t, int64_t dx_stride_h,
+                     void* dweight, void* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Losses that keep a router balanced and its logits small (the paper names none; this is the usual pair for a softmax router), over the n tokens that
+ * are valid:  p = softmax(logits[t, :]),  counts[e] = #{valid t, j : topk_idx[t, j] == e},  importance[e] = 1/n sum_t p[t, e],
+ *   losses[0] = E / (k n) sum_e counts[e] importance[e]   (1 when all experts are chosen alike),   losses[1] = 1/n sum_t lse[t]^2,
+ *   lse[t] = log sum_e exp(logits[t, e]), 0 for a token that is not valid.  n == 0: losses and importance are 0.
+ *   logits [T, E] f32; topk_idx [T, k] i32 (from moe_route_topk; an index outside [0, E) is not counted); valid [T] u8 (0: padding), or NULL: all valid.
+ *   The logits of a token that is not valid are not read.
+ *   losses [2] f32, counts [E + 1] i32 with counts[E] = n, importance [E] f32, lse [T] f32: out.
+ *   A logit of -inf has no probability; a row of nothing else counts as a token, with no probabilities, lse = -inf and no part in losses[1].
+ * Backward of balance dlosses[0] losses[0] + z dlosses[1] losses[1], the counts being constants:
+ *   dlogits[t, e] = add[t, e] + p[t, e] (balance dlosses[0] / n (s_e - sum_e' s_e' p[t, e']) + z dlosses[1] 2 / n lse[t]),  s_e = E counts[e] / (k n),
+ *   and add[t, e] alone for a token that is not valid.
+ *   counts and lse as the forward call wrote them; dlosses [2] f32 (device), or NULL: ones; add [T, E] f32 (e.g. from moe_route_topk_bwd; may be
+ *   dlogits), or NULL: zeros; dlogits [T, E] f32 out, every element written.
+ * The order of all sums depends on the sizes only.  Limits as for moe_route_topk; all tensors but valid 16-byte aligned.
+ */
+size_t moe_balance_loss_fwd_workspace_bytes(int T, int E, int k);
+int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int E, int k, float* losses,
+                             int32_t* counts, float* importance, float* lse, void* ws, size_t ws_bytes, void* stream);
+int32_t moe_balance_loss_bwd(const float* logits, const int32_t* counts, const float* lse, const uint8_t* valid, int T, int E, int k,
+                             float balance, float z, const float* dlosses, const float* add, float* dlogits, void* stream);
+
 /* ---------------------------------------------------------------------------------------
  * Paged key/value cache for generation (a widening beyond the paper, which trains).
  * A page holds page_size consecutive tokens of one sequence, for all key/value heads:
@@ -345,6 +411,13 @@ int32_t moe_kv_cache_write(const moe_kv_cache_t* cache, const void* k, int64_t k
                            int64_t q_stride_t, int64_t q_stride_h, int Hq, int rot, const int32_t* positions,
                            const float* cos, const float* sin, int n_pos, int interleaved, void* q_out,
                            int64_t qo_stride_t, int64_t qo_stride_h, void* stream);
+
+/* The same with positions of several axes, as in moe_rope_axes_fwd. */
+int32_t moe_kv_cache_write_axes(const moe_kv_cache_t* cache, const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v,
+                                int64_t v_stride_t, int64_t v_stride_h, int T, const int64_t* slots, const void* q,
+                                int64_t q_stride_t, int64_t q_stride_h, int Hq, int rot, const int32_t* positions, int n_axes,
+                                const uint8_t* pair_axis, const float* cos, const float* sin, int n_pos, int interleaved, void* q_out,
+                                int64_t qo_stride_t, int64_t qo_stride_h, void* stream);
 
 /* Cached keys and values back into packed rows: row r in [row_start[b], row_start[b+1]) is token first[b] + r - row_start[b]
  * of sequence b (first == NULL: from its first token on).

@@ -11,7 +11,7 @@ LIB = os.path.join(PKG, "libmoe_gfx950.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
-SOURCES = ["api.hip", "route.hip", "permute.hip", "gemm_f32.hip", "gemm_bf16.hip", "rope.hip", "attn_decode.hip"]
+SOURCES = ["api.hip", "route.hip", "permute.hip", "gemm_f32.hip", "gemm_bf16.hip", "rope.hip", "attn_decode.hip", "norm.hip", "balance.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -19,69 +19,23 @@
 #include "launch_plan.h"
 #include "moe_common.h"
 #include "mx8_codes.h"
+#include "pieces.h"
 
 namespace moe {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kAtOnce = 4;                             // head rows whose loads a lane has in flight
 constexpr int kBlocksWanted = 4096;                    // 8192 tokens of 36 heads: 29.1 us, 30.3 for 2048 and 29.6 for 8192; reads: 38.0, 38.7 for 1
+constexpr int kMaxRopeAxes = 4, kMaxRopePairs = 256;   // two bits each; heads have up to 512 elements
 constexpr int kMaxBlocksX = 1 << 20;                   // a workgroup walks on where there are more tokens
 
 __device__ __forceinline__ int wave_of_block() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6); }
 
-// N consecutive elements of a head row as they lie in memory: 16 bytes, or 32 in fp32 rows of more than 64 pieces of 16.
-template <class E, int N> struct Piece;
-template <> struct Piece<bf16_t, 8> {
-  u32x4 w;
-  __device__ __forceinline__ void load(const bf16_t* p) { w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
-  __device__ __forceinline__ void store(bf16_t* p) const { __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p)); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) { v[2 * q] = bf16_lo(w[q]); v[2 * q + 1] = bf16_hi(w[q]); }
-  }
-  __device__ __forceinline__ void set(const float (&v)[8]) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
-  }
-  __device__ __forceinline__ Piece of_lane(int lane) const {
-    Piece o;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) o.w[q] = __shfl(w[q], lane, 64);
-    return o;
-  }
-};
-template <int N> struct Piece<float, N> {
-  f32x4 w[N / 4];
-  __device__ __forceinline__ void load(const float* p) {
-#pragma unroll
-    for (int g = 0; g < N / 4; ++g) w[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + g);
-  }
-  __device__ __forceinline__ void store(float* p) const {
-#pragma unroll
-    for (int g = 0; g < N / 4; ++g) __builtin_nontemporal_store(w[g], reinterpret_cast<f32x4*>(p) + g);
-  }
-  __device__ __forceinline__ void get(float (&v)[N]) const {
-#pragma unroll
-    for (int q = 0; q < N; ++q) v[q] = w[q / 4][q % 4];
-  }
-  __device__ __forceinline__ void set(const float (&v)[N]) {
-#pragma unroll
-    for (int q = 0; q < N; ++q) w[q / 4][q % 4] = v[q];
-  }
-  __device__ __forceinline__ Piece of_lane(int lane) const {
-    Piece o;
-#pragma unroll
-    for (int q = 0; q < N; ++q) o.w[q / 4][q % 4] = __shfl(w[q / 4][q % 4], lane, 64);
-    return o;
-  }
-};
 // N table values, or one for every two
 template <int N> __device__ __forceinline__ void load_table(float (&v)[N], const float* p) {
   if constexpr (N >= 4) {
@@ -98,12 +52,45 @@ template <int N> __device__ __forceinline__ void load_table(float (&v)[N], const
   }
 }
 
+// ---- positions with several axes ---------------------------------------------------------------------------
+// Pair i turns by the position on its axis, positions[axis_i, t].  Which axis is two bits a pair, in the kernel's arguments; a lane looks its pairs'
+// up once.  Where all pairs of every lane share an axis (`whole`) the lane's part of the table is contiguous as ever, else its pairs are fetched one by one.
+struct OneAxis {};
+struct ManyAxes {
+  int n, whole;
+  uint32_t bits[kMaxRopePairs / 16];
+};
+// the axes of n consecutive pairs from `pair` on (a multiple of n, which divides 16)
+__device__ __forceinline__ uint32_t axes_of(const ManyAxes& x, int pair) { return x.bits[pair / 16] >> (2 * (pair % 16)); }
+
+// N/2 or N table values of a lane's pairs
+template <int M> __device__ __forceinline__ void load_axes(float (&c)[M], float (&s)[M], const RotateArgs& a, const ManyAxes& x, uint32_t axes, int pair, long t, int half) {
+  const ScalarInts positions = scalar_ints(a.positions);
+  int p[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = min(max(positions[static_cast<long>(min(i, x.n - 1)) * a.T + t], 0), a.n_pos - 1);
+  auto row = [&](uint32_t axis) { const int lo = axis & 1 ? p[1] : p[0], hi = axis & 1 ? p[3] : p[2]; return static_cast<long>(axis & 2 ? hi : lo) * half + pair; };
+  if (x.whole) {
+    const long at = row(axes);
+    load_table(c, a.cos + at);
+    load_table(s, a.sin + at);
+  } else {
+#pragma unroll
+    for (int q = 0; q < M; ++q) {
+      const long at = row(axes >> (2 * q)) + q;
+      c[q] = a.cos[at];
+      s[q] = a.sin[at];
+    }
+  }
+}
+
 // ---- the turn, with or without a cache behind it ----------------------------------------------------------
 // A wave has one token at a time and walks its head rows, 64 / lanes of them next to each other in memory per access and kAtOnce
 // accesses in flight.  (A wave over as many tokens instead, a head
 // row of each, moves 256-byte pieces: 40960 tokens of 32 + 4 heads 142 us, as it is 124.)
-template <class E, int N, int CACHE /* 0: none, 1: elements as they are, 2: 8-bit blocks */>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lanes, int heads_per_block) {
+template <class E, int N, int CACHE /* 0: none, 1: elements as they are, 2: 8-bit blocks */, class Axes>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, Axes axes, int lanes, int heads_per_block) {
+  constexpr bool kMany = std::is_same_v<Axes, ManyAxes>;
   const int lane = static_cast<int>(threadIdx.x) & 63, chunk = lane & (lanes - 1), sub = lane / lanes, abreast = 64 / lanes;
   if (chunk * N >= a.D) return;                        // lanes of the power of two that a head row has no elements for
   const int half = a.rot / 2;
@@ -111,25 +98,35 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int lane
   const int partner = !turned ? lane : first ? lane + half / N : lane - half / N;
   const int turned_rows = a.Hq + a.Hk, rows = turned_rows + a.Hv;
   const int h0 = blockIdx.y * heads_per_block, h1 = min(rows, h0 + heads_per_block);
+  const int pair = a.interleaved ? chunk * (N / 2) : first ? chunk * N : chunk * N - half;   // the first of the lane's
+  uint32_t mine = 0;
+  if constexpr (kMany) mine = turned ? axes_of(axes, pair) : 0;
 
   for (long t = static_cast<long>(blockIdx.x) * kWaves + wave_of_block(); t < a.T; t += static_cast<long>(gridDim.x) * kWaves) {
     float co[N], si[N];
     if (turned && h0 < turned_rows) {
-      const int p = min(max(a.positions[t], 0), a.n_pos - 1);
+      long at = 0;
+      if constexpr (!kMany) at = static_cast<long>(min(max(a.positions[t], 0), a.n_pos - 1)) * half + pair;
       if (a.interleaved) {
-        const long at = static_cast<long>(p) * half + chunk * (N / 2);
         float c[N / 2], s[N / 2];
-        load_table(c, a.cos + at);
-        load_table(s, a.sin + at);
+        if constexpr (kMany) {
+          load_axes(c, s, a, axes, mine, pair, t, half);
+        } else {
+          load_table(c, a.cos + at);
+          load_table(s, a.sin + at);
+        }
 #pragma unroll
         for (int q = 0; q < N; ++q) {
           co[q] = c[q / 2];
           si[q] = (q % 2 == 0) == (a.back != 0) ? s[q / 2] : -s[q / 2];
         }
       } else {
-        const long at = static_cast<long>(p) * half + (first ? chunk * N : chunk * N - half);
-        load_table(co, a.cos + at);
-        load_table(si, a.sin + at);
+        if constexpr (kMany) {
+          load_axes(co, si, a, axes, mine, pair, t, half);
+        } else {
+          load_table(co, a.cos + at);
+          load_table(si, a.sin + at);
+        }
 #pragma unroll
         for (int q = 0; q < N; ++q) si[q] = first == (a.back != 0) ? si[q] : -si[q];
       }
@@ -217,13 +214,13 @@ int lanes_of_row(int D, int n) {
   return lanes;
 }
 
-template <class E, int N, int CACHE> void launch_rotate(const char* name, const RotateArgs& a) {
+template <class E, int N, int CACHE, class Axes> void launch_rotate(const char* name, const RotateArgs& a, const Axes& axes) {
   const int lanes = lanes_of_row(a.D, N), step = 64 / lanes * kAtOnce, rows = a.Hq + a.Hk + a.Hv;
   const int bx = static_cast<int>(a.T / kWaves + (a.T % kWaves != 0)), gx = bx < kMaxBlocksX ? bx : kMaxBlocksX;
   // heads are cut into as many blocks as it takes to have kBlocksWanted workgroups; a block is a multiple of what a wave has in flight
   const int want = ceil_div(kBlocksWanted, gx), most = ceil_div(rows, step), cut = want < most ? want : most;
   const int heads = ceil_div(ceil_div(rows, cut), step) * step;
-  MOE_LAUNCH(name, (rotate_kernel<E, N, CACHE>), dim3(gx, ceil_div(rows, heads)), dim3(kThreads), 0, a.stream, a, lanes, heads);
+  MOE_LAUNCH(name, (rotate_kernel<E, N, CACHE, Axes>), dim3(gx, ceil_div(rows, heads)), dim3(kThreads), 0, a.stream, a, axes, lanes, heads);
 }
 
 // ---- back from the pages ----------------------------------------------------------------------------------
@@ -337,10 +334,23 @@ int32_t check_heads(const char* who, int dtype, int T, int D, int rot) {
   return MOE_OK;
 }
 
+// pair_axis [rot / 2] as the kernel takes it, for lanes of n elements
+int32_t take_axes(const char* who, int n_axes, const uint8_t* pair_axis, int rot, int interleaved, int n, ManyAxes* out) {
+  MOE_REQUIRE(rot == 0 || pair_axis, MOE_ERR_INVALID_ARG, "%s: a rotation needs the axis of every pair", who);
+  const int per_lane = interleaved ? n / 2 : n;
+  *out = ManyAxes{n_axes, 1, {}};
+  for (int i = 0; i < rot / 2; ++i) {
+    MOE_REQUIRE(pair_axis[i] < n_axes, MOE_ERR_INVALID_ARG, "%s: pair %d is on axis %d of %d", who, i, pair_axis[i], n_axes);
+    out->bits[i / 16] |= static_cast<uint32_t>(pair_axis[i]) << (2 * (i % 16));
+    if (pair_axis[i] != pair_axis[i / per_lane * per_lane]) out->whole = 0;
+  }
+  return MOE_OK;
+}
+
 int32_t rope(const char* who, const char* name, int back, const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k, int64_t k_stride_t,
              int64_t k_stride_h, int dtype, int T, int Hq, int Hk, int D, int rot, const int32_t* positions, const float* cos, const float* sin,
              int n_pos, int interleaved, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* k_out, int64_t ko_stride_t, int64_t ko_stride_h,
-             void* stream) {
+             void* stream, int n_axes = 0, const uint8_t* pair_axis = nullptr) {
   if (int32_t rc = check_heads(who, dtype, T, D, rot)) return rc;
   MOE_REQUIRE(Hq >= 0 && Hk >= 0 && Hq + static_cast<int64_t>(Hk) > 0 && Hq + static_cast<int64_t>(Hk) <= 65536, MOE_ERR_INVALID_ARG, "%s: heads Hq=%d Hk=%d", who, Hq, Hk);
   if (T == 0) return MOE_OK;
@@ -356,10 +366,17 @@ int32_t rope(const char* who, const char* name, int back, const void* q, int64_t
   a.T = T; a.Hq = Hq; a.Hk = Hk; a.Hv = 0; a.D = D; a.rot = rot; a.positions = positions; a.cos = cos; a.sin = sin; a.n_pos = n_pos;
   a.interleaved = interleaved != 0; a.back = back; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.k_out = k_out; a.ko_stride_t = ko_stride_t; a.ko_stride_h = ko_stride_h; a.stream = static_cast<hipStream_t>(stream);
+  const bool many = n_axes != 0;
+  ManyAxes axes{};
+  if (many)
+    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_BF16 || D > 256 ? 8 : 4, &axes)) return rc;
+  auto launch = [&](auto x) {
+    if (dtype == MOE_BF16) launch_rotate<bf16_t, 8, 0>(name, a, x);
+    else if (D <= 256) launch_rotate<float, 4, 0>(name, a, x);
+    else launch_rotate<float, 8, 0>(name, a, x);
+  };
   begin_call(who, a.stream);
-  if (dtype == MOE_BF16) launch_rotate<bf16_t, 8, 0>(name, a);
-  else if (D <= 256) launch_rotate<float, 4, 0>(name, a);
-  else launch_rotate<float, 8, 0>(name, a);
+  if (many) launch(axes); else launch(OneAxis{});
   return end_call();
 }
 
@@ -421,34 +438,81 @@ extern "C" int32_t moe_rope_bwd(const void* dq, int64_t q_stride_t, int64_t q_st
               interleaved, dq_in, qo_stride_t, qo_stride_h, dk_in, ko_stride_t, ko_stride_h, stream);
 }
 
-extern "C" int32_t moe_kv_cache_write(const moe_kv_cache_t* cache, const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v,
+static int32_t cache_write(const char* who, const char* entry, const moe_kv_cache_t* cache, const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v,
                                       int64_t v_stride_t, int64_t v_stride_h, int T, const int64_t* slots, const void* q, int64_t q_stride_t,
                                       int64_t q_stride_h, int Hq, int rot, const int32_t* positions, const float* cos, const float* sin, int n_pos,
-                                      int interleaved, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* stream) {
-  if (int32_t rc = check_cache("kv_cache_write", cache)) return rc;
+                                      int interleaved, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* stream, int n_axes = 0, const uint8_t* pair_axis = nullptr) {
+  if (int32_t rc = check_cache(who, cache)) return rc;
   const int dtype = cache->dtype == MOE_F32 ? MOE_F32 : MOE_BF16;
-  if (int32_t rc = check_heads("kv_cache_write", dtype, T, cache->dim, rot)) return rc;
-  MOE_REQUIRE(Hq >= 0 && Hq <= 65536, MOE_ERR_INVALID_ARG, "kv_cache_write: Hq=%d", Hq);
+  if (int32_t rc = check_heads(who, dtype, T, cache->dim, rot)) return rc;
+  MOE_REQUIRE(Hq >= 0 && Hq <= 65536, MOE_ERR_INVALID_ARG, "%s: Hq=%d", who, Hq);
   if (T == 0) return MOE_OK;
-  MOE_REQUIRE(k && v && slots && (Hq == 0 || (q && q_out)), MOE_ERR_INVALID_ARG, "kv_cache_write: null pointer");
-  MOE_REQUIRE(rot == 0 || (positions && cos && sin && n_pos > 0), MOE_ERR_INVALID_ARG, "kv_cache_write: a rotation needs positions and a table (n_pos=%d)", n_pos);
+  MOE_REQUIRE(k && v && slots && (Hq == 0 || (q && q_out)), MOE_ERR_INVALID_ARG, "%s: null pointer", who);
+  MOE_REQUIRE(rot == 0 || (positions && cos && sin && n_pos > 0), MOE_ERR_INVALID_ARG, "%s: a rotation needs positions and a table (n_pos=%d)", who, n_pos);
   MOE_REQUIRE(aligned16(k) && aligned16(v) && aligned16(q) && aligned16(q_out) && aligned16(cos) && aligned16(sin), MOE_ERR_INVALID_ARG,
-              "kv_cache_write: tensors must be 16-byte aligned");
+              "%s: tensors must be 16-byte aligned", who);
   MOE_REQUIRE(strides_ok(dtype, k_stride_t, k_stride_h) && strides_ok(dtype, v_stride_t, v_stride_h) &&
               (Hq == 0 || (strides_ok(dtype, q_stride_t, q_stride_h) && strides_ok(dtype, qo_stride_t, qo_stride_h))), MOE_ERR_INVALID_ARG,
-              "kv_cache_write: strides must be multiples of 16 bytes");
+              "%s: strides must be multiples of 16 bytes", who);
   RotateArgs a{};
   a.q = q; a.q_stride_t = q_stride_t; a.q_stride_h = q_stride_h; a.k = k; a.k_stride_t = k_stride_t; a.k_stride_h = k_stride_h;
   a.v = v; a.v_stride_t = v_stride_t; a.v_stride_h = v_stride_h;
   a.T = T; a.Hq = Hq; a.Hk = a.Hv = cache->heads; a.D = cache->dim; a.rot = rot; a.positions = positions; a.cos = cos; a.sin = sin; a.n_pos = n_pos;
   a.interleaved = interleaved != 0; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.slots = slots; a.cache = *cache; a.stream = static_cast<hipStream_t>(stream);
-  begin_call("moe_kv_cache_write", a.stream);
-  if (cache->dtype == MOE_F32) launch_rotate<float, 4, 1>("kv_cache_write", a);
-  else if (cache->dtype == MOE_BF16) launch_rotate<bf16_t, 8, 1>("kv_cache_write", a);
-  else launch_rotate<bf16_t, 8, 2>("kv_cache_write", a);
+  const bool many = n_axes != 0;
+  ManyAxes axes{};
+  if (many)
+    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_F32 ? 4 : 8, &axes)) return rc;
+  auto launch = [&](auto x) {
+    if (cache->dtype == MOE_F32) launch_rotate<float, 4, 1>(who, a, x);
+    else if (cache->dtype == MOE_BF16) launch_rotate<bf16_t, 8, 1>(who, a, x);
+    else launch_rotate<bf16_t, 8, 2>(who, a, x);
+  };
+  begin_call(entry, a.stream);
+  if (many) launch(axes); else launch(OneAxis{});
   return end_call();
 }
+
+extern "C" int32_t moe_kv_cache_write(const moe_kv_cache_t* cache, const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v,
+                                      int64_t v_stride_t, int64_t v_stride_h, int T, const int64_t* slots, const void* q, int64_t q_stride_t,
+                                      int64_t q_stride_h, int Hq, int rot, const int32_t* positions, const float* cos, const float* sin, int n_pos,
+                                      int interleaved, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* stream) {
+  return cache_write("kv_cache_write", "moe_kv_cache_write", cache, k, k_stride_t, k_stride_h, v, v_stride_t, v_stride_h, T, slots, q, q_stride_t, q_stride_h, Hq, rot,
+                     positions, cos, sin, n_pos, interleaved, q_out, qo_stride_t, qo_stride_h, stream);
+}
+
+// An axis count that is none is refused here: 0 stands for positions without axes above.
+#define MOE_REQUIRE_AXES(who) \
+  MOE_REQUIRE(n_axes >= 1 && n_axes <= kMaxRopeAxes, MOE_ERR_INVALID_ARG, "%s: %d axes, 1 to %d are possible", who, n_axes, kMaxRopeAxes)
+
+extern "C" int32_t moe_kv_cache_write_axes(const moe_kv_cache_t* cache, const void* k, int64_t k_stride_t, int64_t k_stride_h, const void* v,
+                                           int64_t v_stride_t, int64_t v_stride_h, int T, const int64_t* slots, const void* q, int64_t q_stride_t,
+                                           int64_t q_stride_h, int Hq, int rot, const int32_t* positions, int n_axes, const uint8_t* pair_axis, const float* cos,
+                                           const float* sin, int n_pos, int interleaved, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* stream) {
+  MOE_REQUIRE_AXES("kv_cache_write_axes");
+  return cache_write("kv_cache_write_axes", "moe_kv_cache_write_axes", cache, k, k_stride_t, k_stride_h, v, v_stride_t, v_stride_h, T, slots, q, q_stride_t, q_stride_h, Hq,
+                     rot, positions, cos, sin, n_pos, interleaved, q_out, qo_stride_t, qo_stride_h, stream, n_axes, pair_axis);
+}
+
+extern "C" int32_t moe_rope_axes_fwd(const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k, int64_t k_stride_t, int64_t k_stride_h, int dtype,
+                                     int T, int Hq, int Hk, int D, int rot, const int32_t* positions, int n_axes, const uint8_t* pair_axis, const float* cos,
+                                     const float* sin, int n_pos, int interleaved, void* q_out, int64_t qo_stride_t, int64_t qo_stride_h, void* k_out,
+                                     int64_t ko_stride_t, int64_t ko_stride_h, void* stream) {
+  MOE_REQUIRE_AXES("moe_rope_axes_fwd");
+  return rope("moe_rope_axes_fwd", "rope_axes_fwd", 0, q, q_stride_t, q_stride_h, k, k_stride_t, k_stride_h, dtype, T, Hq, Hk, D, rot, positions, cos, sin, n_pos,
+              interleaved, q_out, qo_stride_t, qo_stride_h, k_out, ko_stride_t, ko_stride_h, stream, n_axes, pair_axis);
+}
+
+extern "C" int32_t moe_rope_axes_bwd(const void* dq, int64_t q_stride_t, int64_t q_stride_h, const void* dk, int64_t k_stride_t, int64_t k_stride_h, int dtype,
+                                     int T, int Hq, int Hk, int D, int rot, const int32_t* positions, int n_axes, const uint8_t* pair_axis, const float* cos,
+                                     const float* sin, int n_pos, int interleaved, void* dq_in, int64_t qo_stride_t, int64_t qo_stride_h, void* dk_in,
+                                     int64_t ko_stride_t, int64_t ko_stride_h, void* stream) {
+  MOE_REQUIRE_AXES("moe_rope_axes_bwd");
+  return rope("moe_rope_axes_bwd", "rope_axes_bwd", 1, dq, q_stride_t, q_stride_h, dk, k_stride_t, k_stride_h, dtype, T, Hq, Hk, D, rot, positions, cos, sin, n_pos,
+              interleaved, dq_in, qo_stride_t, qo_stride_h, dk_in, ko_stride_t, ko_stride_h, stream, n_axes, pair_axis);
+}
+#undef MOE_REQUIRE_AXES
 
 extern "C" int32_t moe_kv_cache_read(const moe_kv_cache_t* cache, const int32_t* block_table, int max_pages, const int32_t* row_start,
                                      const int32_t* first, int B, int rows, void* k_out, void* v_out, void* stream) {

@@ -34,6 +34,9 @@ EXPORTS = [
     "moe_grouped_gemm_down_mx8",
     "moe_rope_table", "moe_rope_fwd", "moe_rope_bwd", "moe_kv_cache_write", "moe_kv_cache_read",
     "moe_paged_attn_decode_workspace_bytes", "moe_paged_attn_decode",
+    "moe_rope_axes_fwd", "moe_rope_axes_bwd", "moe_kv_cache_write_axes",
+    "moe_norm_fwd", "moe_norm_bwd_workspace_bytes", "moe_norm_bwd",
+    "moe_balance_loss_fwd_workspace_bytes", "moe_balance_loss_fwd", "moe_balance_loss_bwd",
     "moe_set_launch_hook",
 ]
 
@@ -134,6 +137,24 @@ def _load():
     lib.moe_paged_attn_decode_workspace_bytes.argtypes = [i32] * 6
     lib.moe_paged_attn_decode.restype = ctypes.c_int32
     lib.moe_paged_attn_decode.argtypes = [vp, i64, i64, vp, vp, i32, vp, i32, i32, f32, i32, vp, vp, vp, sz, vp]
+    for turn in (lib.moe_rope_axes_fwd, lib.moe_rope_axes_bwd):
+        turn.restype = ctypes.c_int32
+        turn.argtypes = [vp, i64, i64] * 2 + [i32] * 6 + [vp, i32, vp] + [vp] * 2 + [i32] * 2 + [vp, i64, i64] * 2 + [vp]
+    lib.moe_kv_cache_write_axes.restype = ctypes.c_int32
+    lib.moe_kv_cache_write_axes.argtypes = ([vp] + [vp, i64, i64] * 2 + [i32, vp] + [vp, i64, i64] + [i32] * 2 + [vp, i32, vp] + [vp] * 2 + [i32] * 2 +
+                                            [vp, i64, i64, vp])
+    lib.moe_norm_fwd.restype = ctypes.c_int32
+    lib.moe_norm_fwd.argtypes = [vp, i64, i64] * 2 + [i32] * 5 + [vp, vp, i32, f32] + [vp, i64, i64] * 2 + [vp] * 3
+    lib.moe_norm_bwd_workspace_bytes.restype = sz
+    lib.moe_norm_bwd_workspace_bytes.argtypes = [i32] * 3
+    lib.moe_norm_bwd.restype = ctypes.c_int32
+    lib.moe_norm_bwd.argtypes = [vp, i64, i64] * 2 + [i32] * 4 + [vp] * 3 + [i32] + [vp, i64, i64] * 2 + [vp] * 3 + [sz, vp]
+    lib.moe_balance_loss_fwd_workspace_bytes.restype = sz
+    lib.moe_balance_loss_fwd_workspace_bytes.argtypes = [i32] * 3
+    lib.moe_balance_loss_fwd.restype = ctypes.c_int32
+    lib.moe_balance_loss_fwd.argtypes = [vp] * 3 + [i32] * 3 + [vp] * 5 + [sz, vp]
+    lib.moe_balance_loss_bwd.restype = ctypes.c_int32
+    lib.moe_balance_loss_bwd.argtypes = [vp] * 4 + [i32] * 3 + [f32] * 2 + [vp] * 4
     lib.moe_set_launch_hook.restype = ctypes.c_int32
     lib.moe_set_launch_hook.argtypes = [LAUNCH_HOOK, vp]
     return lib
@@ -693,3 +714,230 @@ def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None,
     _check(lib.moe_paged_attn_decode(*qi, ref, pages.data_ptr(), pages.shape[1], lens.data_ptr(), B, Hq, scale, window, out.data_ptr(), _ptr(lse),
                                      ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
     return out, lse
+
+
+# ---- positions with several axes, the norm, the router's losses ------------------------------------------------------
+# These refuse tensors that are not on the current device, whose stream the call goes to.
+
+def _on(t, name):
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.get_device() != _current_device():
+        raise ValueError("%s is not on the current device" % name)
+    return t
+
+
+def _flat(t, dtype, n, name):
+    """The pointer of a contiguous tensor of n elements on the current device (None: null)."""
+    if t is None:
+        return None
+    _need(_on(t, name), dtype, name)
+    if n is not None and t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    return t.data_ptr()
+
+
+def _axes(positions, cos, sin, pair_axis, T):
+    if not isinstance(pair_axis, bytes):
+        raise TypeError("pair_axis must be bytes, the axis of every pair")
+    if positions is None or cos is None or sin is None:
+        raise ValueError("positions, cos and sin must be given")
+    at = _flat(positions, torch.int32, None, "positions"), _flat(cos, torch.float32, None, "cos"), _flat(sin, torch.float32, None, "sin")
+    if cos.dim() != 2 or sin.shape != cos.shape or positions.dim() != 2 or positions.shape[1] != T:
+        raise ValueError("cos and sin must be [n_pos, rot / 2] and positions [axes, %d]" % T)
+    if len(pair_axis) != cos.shape[1]:
+        raise ValueError("pair_axis must have one entry per pair")
+    return at[0], positions.shape[0], pair_axis, at[1], at[2], cos.shape[0], 2 * cos.shape[1]
+
+
+def _rope_axes(back, q, k, positions, cos, sin, pair_axis, interleaved, out):
+    if out is None:
+        out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+    if _marshal is not None:
+        _check(_marshal.rope_axes(back, q, k, positions, cos, sin, pair_axis, interleaved, out[0], out[1], _stream(), _current_device()))
+        return out
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q or k must be given")
+    code, (T, _, D) = _dtype_code(some), some.shape
+    qi = qo = ki = ko = _NO_HEADS
+    Hq = Hk = 0
+    if q is not None:
+        Hq = q.shape[1]
+        qi, qo = _heads(_on(q, "q"), some.dtype, "q"), _heads(_on(out[0], "q out"), some.dtype, "q out", q.shape)
+    if k is not None:
+        Hk = k.shape[1]
+        ki, ko = _heads(_on(k, "k"), some.dtype, "k", (T, Hk, D)), _heads(_on(out[1], "k out"), some.dtype, "k out", k.shape)
+    p_pos, n_axes, pairs, p_cos, p_sin, n_pos, rot = _axes(positions, cos, sin, pair_axis, T)
+    call = lib.moe_rope_axes_bwd if back else lib.moe_rope_axes_fwd
+    _check(call(*qi, *ki, code, T, Hq, Hk, D, rot, p_pos, n_axes, pairs, p_cos, p_sin, n_pos, interleaved, *qo, *ko, _stream()))
+    return out
+
+
+def moe_rope_axes_fwd(q, k, positions, cos, sin, pair_axis, interleaved=False, out=None):
+    """moe_rope_fwd with positions [axes, T] i32 of up to four axes; pair_axis: bytes, the axis of each of the rot / 2 pairs (generation.rope_axes).
+    -> q_out, k_out; out = (q, k) rotates in place."""
+    return _rope_axes(False, q, k, positions, cos, sin, pair_axis, interleaved, out)
+
+
+def moe_rope_axes_bwd(dq, dk, positions, cos, sin, pair_axis, interleaved=False, out=None):
+    """Gradients of moe_rope_axes_fwd's inputs from those of its outputs."""
+    return _rope_axes(True, dq, dk, positions, cos, sin, pair_axis, interleaved, out)
+
+
+def moe_kv_cache_write_axes(cache, k, v, slots, q, positions, cos, sin, pair_axis, interleaved=False, q_out=None):
+    """moe_kv_cache_write with positions [axes, T] i32 and pair_axis as in moe_rope_axes_fwd; q may be None.  -> q_out (None without q)."""
+    ref = cache.ref
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=cache.dtype, device=q.device)
+    if _marshal is not None:
+        _check(_marshal.kv_cache_write_axes(ref, cache.k.get_device(), k, v, slots, q, positions, cos, sin, pair_axis, interleaved, q_out, _stream(), _current_device()))
+        return q_out
+    _on(cache.k, "cache")
+    T, dt = k.shape[0], cache.dtype
+    shape = (T, cache.heads, cache.dim)
+    ki, vi = _heads(_on(k, "k"), dt, "k", shape), _heads(_on(v, "v"), dt, "v", shape)
+    p_slots = _flat(slots, torch.int64, T, "slots")
+    qi = qo = _NO_HEADS
+    Hq = 0
+    if q is not None:
+        Hq = q.shape[1]
+        qi, qo = _heads(_on(q, "q"), dt, "q", (T, Hq, cache.dim)), _heads(_on(q_out, "q_out"), dt, "q_out", q.shape)
+    p_pos, n_axes, pairs, p_cos, p_sin, n_pos, rot = _axes(positions, cos, sin, pair_axis, T)
+    _check(lib.moe_kv_cache_write_axes(ref, *ki, *vi, T, p_slots, *qi, Hq, rot, p_pos, n_axes, pairs, p_cos, p_sin, n_pos, interleaved, *qo, _stream()))
+    return q_out
+
+
+def _rows(t, like, name):
+    """[tokens, dim] or [tokens, heads, dim] whose rows are contiguous: pointer, strides of tokens and heads (None: null)."""
+    if t is None:
+        return _NO_HEADS
+    _on(t, name)
+    if t.dim() not in (2, 3):
+        raise ValueError("%s must be [tokens, dim] or [tokens, heads, dim]" % name)
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] != 1:
+        raise ValueError("%s: the elements of a row must be contiguous" % name)
+    if t.dtype is not like.dtype:
+        raise TypeError("%s has another element type" % name)
+    if t.shape != like.shape:
+        raise ValueError("%s has another shape" % name)
+    return t.data_ptr(), st[0] if t.shape[0] > 1 else 0, st[1] if t.dim() == 3 and t.shape[1] > 1 else 0
+
+
+def _vectors(D, **named):
+    """The pointers of weights [D] of one type, and its code."""
+    code, out = None, []
+    for name, t in named.items():
+        if t is not None:
+            _on(t, name)
+            c = _dtype_code(t)
+            if code is not None and c != code:
+                raise TypeError("%s has another type than the other weights" % name)
+            if t.shape != (D,) or not t.is_contiguous():
+                raise ValueError("%s must be contiguous, one number per column" % name)
+            code = c
+        out.append(_ptr(t))
+    return out, MOE_F32 if code is None else code
+
+
+def moe_norm_fwd(x, weight=None, bias=None, eps=1e-6, rms=False, residual=None, stats=True, out=None):
+    """Layer norm (rms: rms norm) of the rows of x [T, D] or [T, heads, D], or of h = x + residual; weight, bias [D] f32 or bf16 (None: 1 and 0).
+    -> y, h (None without residual), mean (None with rms), rstd f32 (both None where stats is false); out: the four of them, each as above or, for mean and
+    rstd, None."""
+    if out is None:
+        mk = lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        stat = lambda wanted: torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if wanted and stats else None
+        out = mk(), None if residual is None else mk(), stat(not rms), stat(True)
+    y, h, mean, rstd = out
+    if _marshal is not None:
+        _check(_marshal.norm_fwd(x, weight, bias, eps, rms, residual, y, h, mean, rstd, _stream(), _current_device()))
+        return out
+    if x is None or y is None:
+        raise ValueError("x and y must be given")
+    xi, ri, yo, so = _rows(x, x, "x"), _rows(residual, x, "residual"), _rows(y, x, "y"), _rows(h, x, "h")
+    T, H, D = x.shape[0], x.shape[1] if x.dim() == 3 else 1, x.shape[-1]
+    (p_w, p_b), code = _vectors(D, weight=weight, bias=bias)
+    _check(lib.moe_norm_fwd(*xi, *ri, _dtype_code(x), T, H, D, rms, p_w, p_b, code, eps, *so, *yo, _flat(mean, torch.float32, T * H, "mean"),
+                            _flat(rstd, torch.float32, T * H, "rstd"), _stream()))
+    return out
+
+
+def moe_norm_bwd(dy, x, rstd, mean=None, weight=None, add=None, with_weight=True, with_bias=False, out=None, ws=None):
+    """Gradients of moe_norm_fwd: dy and x (what was normed) like its x, rstd and mean as it gave them (mean None: rms norm), add: a gradient of x from elsewhere.
+    -> dx, dweight, dbias [D] in the type of weight (f32 without one; None unless wanted); out: the three of them."""
+    if out is None:
+        kind = torch.float32 if weight is None else weight.dtype
+        vec = lambda wanted: torch.empty(x.shape[-1], dtype=kind, device=x.device) if wanted else None
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device), vec(with_weight), vec(with_bias)
+    dx, dweight, dbias = out
+    T, H, D = x.shape[0], x.shape[1] if x.dim() == 3 else 1, x.shape[-1]
+    if ws is None and (dweight is not None or dbias is not None):
+        ws, _ = _ws(lib.moe_norm_bwd_workspace_bytes, (T, H, D), None, x.device)
+    if _marshal is not None:
+        _check(_marshal.norm_bwd(dy, x, rstd, mean, weight, add, dx, dweight, dbias, ws, _stream(), _current_device()))
+        return out
+    if dy is None or dx is None or rstd is None:
+        raise ValueError("dy, rstd and dx must be given")
+    di, xi, ai, do = _rows(dy, x, "dy"), _rows(x, x, "x"), _rows(add, x, "add"), _rows(dx, x, "dx")
+    (p_w, p_dw, p_db), code = _vectors(D, weight=weight, dweight=dweight, dbias=dbias)
+    _check(lib.moe_norm_bwd(*di, *xi, _dtype_code(x), T, H, D, _flat(mean, torch.float32, T * H, "mean"), _flat(rstd, torch.float32, T * H, "rstd"), p_w, code, *ai, *do,
+                            p_dw, p_db, _flat(ws, None, None, "ws"), 0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+    return out
+
+
+def _logits(t):
+    if t is None or t.dim() != 2:
+        raise ValueError("logits must be [tokens, experts]")
+    return _flat(t, torch.float32, None, "logits")
+
+
+def _mask(t, n):
+    if t is None:
+        return None
+    if t.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("valid must be bool or uint8")
+    return _flat(t, None, n, "valid")
+
+
+def moe_balance_loss_fwd(logits, topk_idx, valid=None, out=None, ws=None):
+    """Balance loss and z loss of a router: logits [T, E] f32, topk_idx [T, k] i32, valid [T] bool or uint8 (None: all tokens count).
+    -> losses [2] f32, counts [E + 1] i32 (the last one the number of valid tokens), importance [E] f32 (mean probabilities), lse [T] f32."""
+    T, E = logits.shape
+    if out is None:
+        mk = lambda n, t: torch.empty(n, dtype=t, device=logits.device)
+        out = mk(2, torch.float32), mk(E + 1, torch.int32), mk(E, torch.float32), mk(T, torch.float32)
+    losses, counts, importance, lse = out
+    k = topk_idx.shape[-1]
+    if ws is None:
+        ws, _ = _ws(lib.moe_balance_loss_fwd_workspace_bytes, (T, E, k), None, logits.device)
+    if _marshal is not None:
+        _check(_marshal.balance_loss_fwd(logits, topk_idx, valid, losses, counts, importance, lse, ws, _stream(), _current_device()))
+        return out
+    p_logits, p_idx = _logits(logits), _flat(topk_idx, torch.int32, None, "topk_idx")
+    if topk_idx.dim() != 2 or topk_idx.shape[0] != T:
+        raise ValueError("topk_idx must be [tokens, k]")
+    if losses is None or counts is None or importance is None or lse is None:
+        raise ValueError("losses, counts, importance and lse must be given")
+    _check(lib.moe_balance_loss_fwd(p_logits, p_idx, _mask(valid, T), T, E, k, _flat(losses, torch.float32, 2, "losses"), _flat(counts, torch.int32, E + 1, "counts"),
+                                    _flat(importance, torch.float32, E, "importance"), _flat(lse, torch.float32, T, "lse"), _flat(ws, None, None, "ws"),
+                                    ws.numel() * ws.element_size(), _stream()))
+    return out
+
+
+def moe_balance_loss_bwd(logits, counts, lse, k, balance=1.0, z=0.0, dlosses=None, valid=None, add=None, out=None):
+    """Gradient of balance * losses[0] + z * losses[1] (times dlosses [2] f32 on the device, where given) with respect to the logits, counts and lse as
+    moe_balance_loss_fwd gave them, plus add [T, E] (which may be out).  -> dlogits [T, E] f32."""
+    if out is None:
+        out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+    if _marshal is not None:
+        _check(_marshal.balance_loss_bwd(logits, counts, lse, k, balance, z, dlosses, valid, add, out, _stream(), _current_device()))
+        return out
+    p_logits = _logits(logits)
+    T, E = logits.shape
+    if counts is None or lse is None:
+        raise ValueError("counts and lse must be given")
+    _check(lib.moe_balance_loss_bwd(p_logits, _flat(counts, torch.int32, E + 1, "counts"), _flat(lse, torch.float32, T, "lse"), _mask(valid, T), T, E, k, balance, z,
+                                    _flat(dlosses, torch.float32, 2, "dlosses"), _flat(add, torch.float32, T * E, "add"), _flat(out, torch.float32, T * E, "dlogits"),
+                                    _stream()))
+    return out
