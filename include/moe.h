@@ -366,7 +366,7 @@ int32_t moe_norm_bwd(const void* dy, int64_t dy_stride_t, int64_t dy_stride_h, c
  *   losses[0] = E / (k n) sum_e counts[e] importance[e]   (1 when all experts are chosen alike),   losses[1] = 1/n sum_t lse[t]^2,
  *   lse[t] = log sum_e exp(logits[t, e]), 0 for a token that is not valid.  n == 0: losses and importance are 0.
  *   logits [T, E] f32; topk_idx [T, k] i32 (from moe_route_topk; an index outside [0, E) is not counted); valid [T] u8 (0: padding), or NULL: all valid.
- *   The logits of a token that is not valid are not read.
+ *   Logits and indices of a token that is not valid may hold anything.
  *   losses [2] f32, counts [E + 1] i32 with counts[E] = n, importance [E] f32, lse [T] f32: out.
  *   A logit of -inf has no probability; a row of nothing else counts as a token, with no probabilities, lse = -inf and no part in losses[1].
  * Backward of balance dlosses[0] losses[0] + z dlosses[1] losses[1], the counts being constants:

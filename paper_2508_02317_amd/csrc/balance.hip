@@ -14,9 +14,12 @@ namespace moe {
 
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kFwdThreads = 512, kFwdWaves = kFwdThreads / 64, kFwdBlocks = 256;
 constexpr int kBwdThreads = 256, kBwdBlocks = 4096;
-constexpr int kJoinThreads = 1024, kJoinColumns = 256; // of a workgroup at most
+constexpr size_t kHeadBytes = 512;                     // of the workspace: the join's counter and losses
+constexpr int kJoinThreads = 1024, kJoinLanes = 32;    // lanes of a row of sums, at most
 
 struct FwdArgs {
   const float* logits;
@@ -92,15 +95,35 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
   int32_t* counts = reinterpret_cast<int32_t*>(sums + kFwdWaves * a.E);
   const int l = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6, lane = l & (a.lanes - 1), group = static_cast<int>(threadIdx.x) / a.lanes;
   const int groups = kFwdThreads / a.lanes;
+  const long step = static_cast<long>(gridDim.x) * groups;
+  long t = static_cast<long>(blockIdx.x) * groups + group;
+  // what is needed first is requested first: the rows of the first turn, this workgroup's share of the pairs, then the rows of each next turn
+  float v[P][N];
+  uint32_t on;
+  auto fetch = [&](long row) {
+    on = row < a.T ? a.valid ? a.valid[row] : 1u : 0u;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int e = (p * a.lanes + lane) * N;
+#pragma unroll
+      for (int q = 0; q < N; ++q) v[p][q] = -INFINITY;
+      if (row < a.T && e < a.E) load(v[p], a.logits + row * a.E + e);
+    }
+  };
+  fetch(t);
   for (int e = threadIdx.x; e < a.E; e += kFwdThreads) counts[e] = 0;
-  __syncthreads();
   {
-    // pairs of this workgroup's share of the tokens
     const long share = (a.T + static_cast<long>(gridDim.x) - 1) / gridDim.x, first = blockIdx.x * share * a.k, last = min(first + share * a.k, static_cast<long>(a.T) * a.k);
-    for (long i = first + threadIdx.x; i < last; i += kFwdThreads) {
-      const int e = a.topk_idx[i];
-      const bool counted = !a.valid || a.valid[divide(static_cast<uint32_t>(i), a.per_token)];
+    long i = first + threadIdx.x;
+    int e = i < last ? a.topk_idx[i] : -1;
+    uint32_t counted = i < last && a.valid ? a.valid[divide(static_cast<uint32_t>(i), a.per_token)] : 1u;
+    __syncthreads();
+    while (i < last) {
       if (counted && e >= 0 && e < a.E) atomicAdd(&counts[e], 1);
+      i += kFwdThreads;
+      if (i >= last) break;
+      e = a.topk_idx[i];
+      if (a.valid) counted = a.valid[divide(static_cast<uint32_t>(i), a.per_token)];
     }
   }
   float acc[P][N], z_sum = 0.0f;
@@ -109,21 +132,17 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
   for (int p = 0; p < P; ++p)
 #pragma unroll
     for (int q = 0; q < N; ++q) acc[p][q] = 0.0f;
-  for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += static_cast<long>(gridDim.x) * groups) {
-    const long t = base + group;
-    const bool there = t < a.T && (!a.valid || a.valid[t]);
-    float v[P][N], top = -INFINITY;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int e = (p * a.lanes + lane) * N;
-#pragma unroll
-      for (int q = 0; q < N; ++q) v[p][q] = -INFINITY;
-      if (there && e < a.E) load(v[p], a.logits + t * a.E + e);
-    }
+  for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += step, t += step) {
+    const bool there = on != 0;
+    float e[P][N], top = -INFINITY;
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < N; ++q) top = fmaxf(top, v[p][q]);
+      for (int q = 0; q < N; ++q) {
+        e[p][q] = there ? v[p][q] : -INFINITY;         // padding may hold anything
+        top = fmaxf(top, e[p][q]);
+      }
+    if (base + step < a.T) fetch(t + step);
     top = lanes_max(top, a.lanes);
     const float from = top == -INFINITY ? 0.0f : top;  // a row without a finite logit has no probabilities
     float total = 0.0f;
@@ -131,15 +150,15 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
     for (int p = 0; p < P; ++p)
 #pragma unroll
       for (int q = 0; q < N; ++q) {
-        v[p][q] = expf(v[p][q] - from);
-        total += v[p][q];
+        e[p][q] = expf(e[p][q] - from);
+        total += e[p][q];
       }
     total = lanes_sum(total, a.lanes);
     const float scale = total == 0.0f ? 0.0f : 1.0f / total, lse = there ? top + logf(total) : 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < N; ++q) acc[p][q] += v[p][q] * scale;
+      for (int q = 0; q < N; ++q) acc[p][q] += e[p][q] * scale;
     if (lane == 0 && t < a.T) {
       a.lse[t] = lse;
       n += there;
@@ -191,39 +210,57 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
   }
 }
 
-// The workgroups' rows added: `columns` (a power of two) experts a workgroup, kJoinThreads / columns runs of the rows each.  The last workgroup to end,
-// by a counter that the launch before has cleared, adds the losses of all in the order of their numbers.
-__global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, int parts, int columns) {
-  __shared__ float sums[kJoinThreads];
-  __shared__ int32_t counts[kJoinThreads];
-  __shared__ double scratch[2][kJoinThreads / 64];
-  __shared__ int32_t n_all;
-  const int c = static_cast<int>(threadIdx.x) & (columns - 1), run = static_cast<int>(threadIdx.x) / columns, runs = kJoinThreads / columns;
-  const int e = blockIdx.x * columns + c;
-  float sum = 0.0f;
-  int32_t count = 0;
-  if (e < a.E)
-    for (int i = run; i < parts; i += runs) {
-      sum += a.sum_of[static_cast<long>(i) * a.E + e];
-      count += a.count_of[static_cast<long>(i) * a.E + e];
+// The workgroups' rows added: `lanes` (a power of two up to kJoinLanes) lanes of N experts a workgroup, the rows dealt out to kJoinThreads / lanes runs, which are
+// added over a wave and over the waves.  The last workgroup to end, by a counter that the launch before has cleared, adds the losses of all in the order of
+// their numbers.
+template <int N> __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, int parts, int lanes) {
+  constexpr int kWaves = kJoinThreads / 64;
+  __shared__ float sums[kWaves][kJoinLanes * N];
+  __shared__ int32_t counts[kWaves][kJoinLanes * N], n_wave[kWaves];
+  __shared__ double scratch[2][kWaves];
+  const int l = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6, lane = l & (lanes - 1), runs = kJoinThreads / lanes;
+  const int e = (blockIdx.x * lanes + lane) * N;
+  float sum[N] = {};
+  int32_t count[N] = {};
+  if (e < a.E) {
+#pragma unroll 4
+    for (int i = static_cast<int>(threadIdx.x) / lanes; i < parts; i += runs) {
+      const long at = static_cast<long>(i) * a.E + e;
+      if constexpr (N == 4) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(a.sum_of + at);
+        const i32x4 c = *reinterpret_cast<const i32x4*>(a.count_of + at);
+#pragma unroll
+        for (int q = 0; q < N; ++q) { sum[q] += s[q]; count[q] += c[q]; }
+      } else {
+        sum[0] += a.sum_of[at];
+        count[0] += a.count_of[at];
+      }
     }
-  sums[threadIdx.x] = sum;
-  counts[threadIdx.x] = count;
-  if (threadIdx.x < 64) {
-    int n = 0;
-    for (int i = threadIdx.x; i < parts; i += 64) n += a.n_of[i];
-    n = wave_sum_i(n);
-    if (threadIdx.x == 0) n_all = n;
   }
+  int n = 0;
   double z = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kJoinThreads) z += a.z_of[i];
+  for (int i = threadIdx.x; i < parts; i += kJoinThreads) { n += a.n_of[i]; z += a.z_of[i]; }
+  for (int o = lanes; o < 64; o *= 2)
+#pragma unroll
+    for (int q = 0; q < N; ++q) { sum[q] += __shfl_xor(sum[q], o, 64); count[q] += __shfl_xor(count[q], o, 64); }
+  if (l < lanes) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) { sums[wave][lane * N + q] = sum[q]; counts[wave][lane * N + q] = count[q]; }
+  }
+  n = wave_sum_i(n);
+  if (l == 0) n_wave[wave] = n;
   z = block_sum(z, scratch[0]);                        // its barrier stands before the reads below too
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) n += n_wave[w];
   double balance = 0.0;
-  if (run == 0 && e < a.E) {
-    sum = 0.0f;
-    count = 0;
-    for (int r = 0; r < runs; ++r) { sum += sums[r * columns + c]; count += counts[r * columns + c]; }
-    balance = finish_expert(a, e, sum, count, n_all);
+  const int mine = blockIdx.x * lanes * N + threadIdx.x;
+  if (static_cast<int>(threadIdx.x) < lanes * N && mine < a.E) {
+    float s = 0.0f;
+    int32_t c = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) { s += sums[w][threadIdx.x]; c += counts[w][threadIdx.x]; }
+    balance = finish_expert(a, mine, s, c, n);
   }
   balance = block_sum(balance, scratch[1]);
   if (threadIdx.x != 0) return;
@@ -233,53 +270,73 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, i
     balance = 0.0;
     for (unsigned i = 0; i < gridDim.x; ++i) balance += __hip_atomic_load(&a.loss_of[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  finish(a, balance, z, n_all);
+  finish(a, balance, z, n);
 }
 
 template <int N, int P>
 __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
   const int lane = static_cast<int>(threadIdx.x) & (a.lanes - 1), group = static_cast<int>(threadIdx.x) / a.lanes, groups = kBwdThreads / a.lanes;
+  const long step = static_cast<long>(gridDim.x) * groups;
+  long t = static_cast<long>(blockIdx.x) * groups + group;
+  float v[P][N], more[P][N], lse;
+  uint32_t on;
+  auto fetch = [&](long row) {
+    const bool inside = row < a.T;
+    on = inside ? a.valid ? a.valid[row] : 1u : 0u;
+    lse = inside ? a.lse[row] : 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int e = (p * a.lanes + lane) * N;
+#pragma unroll
+      for (int q = 0; q < N; ++q) { v[p][q] = -INFINITY; more[p][q] = 0.0f; }
+      if (inside && e < a.E) {
+        load(v[p], a.logits + row * a.E + e);
+        if (a.add) load(more[p], a.add + row * a.E + e);
+      }
+    }
+  };
+  fetch(t);
   const float many = static_cast<float>(max(a.counts[a.E], 1));
   const float to_balance = a.balance * (a.dlosses ? a.dlosses[0] : 1.0f) / many, to_z = 2.0f * a.z * (a.dlosses ? a.dlosses[1] : 1.0f) / many;
   const float per_pair = static_cast<float>(a.E) / static_cast<float>(a.k) / many;
   float share[P][N];
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+  for (int p = 0; p < P; ++p) {
+    const int e = (p * a.lanes + lane) * N;
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-      const int e = (p * a.lanes + lane) * N + q;
-      share[p][q] = e < a.E ? static_cast<float>(a.counts[e]) * per_pair : 0.0f;
+    for (int q = 0; q < N; ++q) share[p][q] = 0.0f;
+    if (e < a.E) {
+      if constexpr (N == 4) {
+        const i32x4 c = *reinterpret_cast<const i32x4*>(a.counts + e);
+#pragma unroll
+        for (int q = 0; q < N; ++q) share[p][q] = static_cast<float>(c[q]) * per_pair;
+      } else {
+        share[p][0] = static_cast<float>(a.counts[e]) * per_pair;
+      }
     }
-  for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += static_cast<long>(gridDim.x) * groups) {
-    const long t = base + group;
-    const bool there = t < a.T && (!a.valid || a.valid[t]);
-    float v[P][N], out[P][N];
-    const float lse = there ? a.lse[t] : -INFINITY;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int e = (p * a.lanes + lane) * N;
-#pragma unroll
-      for (int q = 0; q < N; ++q) { v[p][q] = -INFINITY; out[p][q] = 0.0f; }
-      if (there && e < a.E) load(v[p], a.logits + t * a.E + e);
-      if (t < a.T && e < a.E && a.add) load(out[p], a.add + t * a.E + e);
-    }
-    const bool any = lse != -INFINITY;                 // else no logit is finite, or the token does not count
-    float mean = 0.0f;
+  }
+  for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += step, t += step) {
+    const bool any = on != 0 && lse != -INFINITY;      // else the token does not count, or has no finite logit
+    const float level = any ? lse * to_z : 0.0f;
+    float e[P][N], out[P][N], sums[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
       for (int q = 0; q < N; ++q) {
-        v[p][q] = any ? expf(v[p][q] - lse) : 0.0f;
-        mean += share[p][q] * v[p][q];
+        e[p][q] = any ? expf(v[p][q] - lse) : 0.0f;
+        out[p][q] = more[p][q];
+        sums[0] += e[p][q];
+        sums[1] += share[p][q] * e[p][q];
       }
-    mean = lanes_sum(mean, a.lanes);
-    const float level = any ? lse * to_z : 0.0f;
+    if (base + step < a.T) fetch(t + step);
+    // the sum of exp(z - lse) is 1 but for the rounding of lse, which dividing by it takes out of the probabilities
+    const float total = lanes_sum(sums[0], a.lanes), scale = total == 0.0f ? 0.0f : 1.0f / total, mean = lanes_sum(sums[1], a.lanes) * scale;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int e = (p * a.lanes + lane) * N;
+      const int c = (p * a.lanes + lane) * N;
 #pragma unroll
-      for (int q = 0; q < N; ++q) out[p][q] += v[p][q] * ((share[p][q] - mean) * to_balance + level);
-      if (t < a.T && e < a.E) store(out[p], a.dlogits + t * a.E + e);
+      for (int q = 0; q < N; ++q) out[p][q] += e[p][q] * scale * ((share[p][q] - mean) * to_balance + level);
+      if (t < a.T && c < a.E) store(out[p], a.dlogits + t * a.E + c);
     }
   }
 }
@@ -329,7 +386,7 @@ extern "C" size_t moe_balance_loss_fwd_workspace_bytes(int T, int E, int k) {
   (void)k;
   if (T < 0 || E <= 0 || E > kMaxExperts) return 0;
   const size_t blocks = fwd_blocks(T, E);
-  return align_up(blocks * (2 * static_cast<size_t>(E) + 2) * 4, 16) + 256;
+  return align_up(blocks * (2 * static_cast<size_t>(E) + 2) * 4, 16) + kHeadBytes;
 }
 
 extern "C" int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int E, int k, float* losses, int32_t* counts,
@@ -344,8 +401,9 @@ extern "C" int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk
   const int blocks = fwd_blocks(T, E);
   FwdArgs a{logits, topk_idx, valid, losses, importance, lse, counts, T, E, k, s.lanes, divisor(k), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   a.joined = static_cast<uint32_t*>(ws);
-  a.loss_of = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);                 // of up to four workgroups
-  a.sum_of = reinterpret_cast<float*>(static_cast<char*>(ws) + 256);
+  a.loss_of = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);                 // of the join's workgroups
+  static_assert(16 + kMaxExperts / kJoinLanes * sizeof(double) <= kHeadBytes);
+  a.sum_of = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeadBytes);
   a.count_of = reinterpret_cast<int32_t*>(a.sum_of + static_cast<size_t>(blocks) * E);
   a.z_of = reinterpret_cast<float*>(a.count_of + static_cast<size_t>(blocks) * E);
   a.n_of = reinterpret_cast<int32_t*>(a.z_of + blocks);
@@ -358,9 +416,11 @@ extern "C" int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk
     else MOE_LAUNCH("balance_fwd", (balance_fwd_kernel<N, P, false>), dim3(blocks), dim3(kFwdThreads), lds, st, a);
   });
   if (blocks > 1) {
-    int columns = 64;
-    while (columns < E && columns < kJoinColumns) columns *= 2;
-    MOE_LAUNCH("balance_join", balance_join_kernel, dim3(ceil_div(E, columns)), dim3(kJoinThreads), 0, st, a, blocks, columns);
+    const int pieces = E / s.width;
+    int lanes = 1;
+    while (lanes < pieces && lanes < kJoinLanes) lanes *= 2;
+    if (s.width == 4) MOE_LAUNCH("balance_join", balance_join_kernel<4>, dim3(ceil_div(pieces, lanes)), dim3(kJoinThreads), 0, st, a, blocks, lanes);
+    else MOE_LAUNCH("balance_join", balance_join_kernel<1>, dim3(ceil_div(pieces, lanes)), dim3(kJoinThreads), 0, st, a, blocks, lanes);
   }
   return end_call();
 }

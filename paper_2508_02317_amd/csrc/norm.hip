@@ -199,7 +199,7 @@ template <class E, int N, int P, int U, bool LAYER>
 __global__ __launch_bounds__(sizeof(E) == 4 ? 1024 : 512) void norm_bwd_kernel(NormArgs a) {
   constexpr int K = LAYER ? 2 : 1;
   __shared__ Sums<U * K> sums;
-  extern __shared__ float columns[];                   // [D] of dw, then of db, on their way from wave to wave
+  extern __shared__ __align__(16) float columns[];     // [half of the waves, or sets of them][D] of dw, then of db: 32 KiB at most
   const Place me(a.lanes, a.waves);
   int turn = 0;
   float w[P][N], dw[P][N], db[P][N];
@@ -278,56 +278,77 @@ __global__ __launch_bounds__(sizeof(E) == 4 ? 1024 : 512) void norm_bwd_kernel(N
       }
     }
   }
-  // the sums over the workgroup's rows: over the groups of a wave, then over the waves (or sets of them) in the order of their numbers
+  // the sums over the workgroup's rows: over the groups of a wave in registers, then over the waves (or sets of them) in the order of their numbers
   const int units = (static_cast<int>(blockDim.x) >> 6) / a.waves, unit = me.wave / a.waves;
+  const bool owner = a.waves > 1 || (static_cast<int>(threadIdx.x) & 63) < a.lanes;
   auto leave = [&](float (&acc)[P][N], float* dst) {
+    for (int o = a.lanes; o < 64; o *= 2) {
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+      for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < N; ++q)
-        for (int o = a.lanes; o < 64; o *= 2) acc[p][q] += __shfl_xor(acc[p][q], o, 64);
-    const bool owner = a.waves > 1 || (static_cast<int>(threadIdx.x) & 63) < a.lanes;
-    for (int i = 0; i < units; ++i) {
-      if (i == unit && owner) {
+        for (int q = 0; q < N; ++q) acc[p][q] += __shfl_xor(acc[p][q], o, 64);
+    }
+    // f(where a piece lies among the D, its four sums at a time)
+    auto pieces = [&](bool who, auto f) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const int column = (p * me.size + me.lane) * N;
-          if (column < a.dim) {
+      for (int p = 0; p < P; ++p) {
+        const int column = (p * me.size + me.lane) * N;
+        if (who && owner && column < a.dim) {
 #pragma unroll
-            for (int q = 0; q < N; ++q) {
-              const float v = i == 0 ? acc[p][q] : columns[column + q] + acc[p][q];
-              if (i + 1 < units) columns[column + q] = v;
-              else dst[column + q] = v;
-            }
-          }
+          for (int q = 0; q < N; q += 4) f(column + q, f32x4{acc[p][q], acc[p][q + 1], acc[p][q + 2], acc[p][q + 3]});
         }
       }
-      __syncthreads();
+    };
+    auto quad = [](float* at) -> f32x4& { return *reinterpret_cast<f32x4*>(at); };
+    if (units == 1) {
+      pieces(true, [&](int c, f32x4 v) { quad(dst + c) = v; });
+      return;
     }
+    // the upper half of the units leaves its sums, the lower half adds its own, all threads add those
+    const int half = units / 2;
+    float* place = columns + (unit % half) * a.dim;
+    pieces(unit >= half, [&](int c, f32x4 v) { quad(place + c) = v; });
+    __syncthreads();
+    pieces(unit < half, [&](int c, f32x4 v) { quad(place + c) += v; });
+    __syncthreads();
+    for (int c = 4 * threadIdx.x; c < a.dim; c += 4 * blockDim.x) {
+      f32x4 v = quad(columns + c);
+      for (int i = 1; i < half; ++i) v += quad(columns + i * a.dim + c);
+      quad(dst + c) = v;
+    }
+    __syncthreads();
   };
   float* mine = a.partial + static_cast<long>(blockIdx.x) * a.dim;
   if (a.want_dw) leave(dw, mine);
   if (a.want_db) leave(db, mine + static_cast<long>(gridDim.x) * a.dim);
 }
 
-// [parts][D] -> [D] in the weights' type, the parts added in their order: kJoinThreads / kJoinColumns runs of them, then the runs
+// [parts][D] -> [D] in the weights' type: a lane has four columns of every kJoinRuns-th part, then the runs are added, over a wave and over the waves.
 __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float* partial, int parts, int dim, void* dweight, void* dbias, int bf16) {
-  constexpr int kRuns = kJoinThreads / kJoinColumns;
-  __shared__ float run[kRuns][kJoinColumns];
-  const int c = static_cast<int>(threadIdx.x) % kJoinColumns, r = static_cast<int>(threadIdx.x) / kJoinColumns, column = blockIdx.x * kJoinColumns + c;
+  constexpr int kQuads = kJoinColumns / 4, kRuns = kJoinThreads / kQuads, kWaves = kJoinThreads / 64;
+  __shared__ float run[kWaves][kJoinColumns];
+  const int c = 4 * (static_cast<int>(threadIdx.x) % kQuads), r = static_cast<int>(threadIdx.x) / kQuads, column = blockIdx.x * kJoinColumns + c;
   const float* src = partial + static_cast<long>(blockIdx.y) * parts * dim;
   void* dst = blockIdx.y ? dbias : dweight;
   if (!dst) return;
-  float v = 0.0f;
-  if (column < dim)
-    for (int i = r; i < parts; i += kRuns) v += src[static_cast<long>(i) * dim + column];
-  run[r][c] = v;
+  f32x4 v = {};
+  if (column < dim) {
+#pragma unroll 4
+    for (int i = r; i < parts; i += kRuns) v += *reinterpret_cast<const f32x4*>(src + static_cast<long>(i) * dim + column);
+  }
+#pragma unroll
+  for (int o = kQuads; o < 64; o *= 2)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] += __shfl_xor(v[q], o, 64);
+  if ((threadIdx.x & 63) < kQuads) *reinterpret_cast<f32x4*>(&run[threadIdx.x >> 6][c]) = v;
   __syncthreads();
-  if (r == 0 && column < dim) {
-    v = 0.0f;
-    for (int i = 0; i < kRuns; ++i) v += run[i][c];
-    if (bf16) static_cast<bf16_t*>(dst)[column] = f32_to_bf16(v);
-    else static_cast<float*>(dst)[column] = v;
+  const int mine = blockIdx.x * kJoinColumns + threadIdx.x;
+  if (threadIdx.x < kJoinColumns && mine < dim) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) sum += run[i][threadIdx.x];
+    if (bf16) static_cast<bf16_t*>(dst)[mine] = f32_to_bf16(sum);
+    else static_cast<float*>(dst)[mine] = sum;
   }
 }
 
@@ -350,7 +371,7 @@ int blocks_of(int rows, const Split& s, int threads, int most) {
 
 template <bool BACK, class E, int N, int P, bool LAYER> void launch_norm(const NormArgs& a, int blocks, int threads, hipStream_t st) {
   if constexpr (BACK)
-    MOE_LAUNCH("norm_bwd", (norm_bwd_kernel<E, N, P, kMaxPieces / P, LAYER>), dim3(blocks), dim3(threads), a.want_dw || a.want_db ? threads / 64 > a.waves ? 4 * a.dim : 0 : 0, st, a);
+    MOE_LAUNCH("norm_bwd", (norm_bwd_kernel<E, N, P, kMaxPieces / P, LAYER>), dim3(blocks), dim3(threads), (a.want_dw || a.want_db) && threads / 64 > a.waves ? threads / 64 / a.waves / 2 * a.dim * 4 : 0, st, a);
   else
     MOE_LAUNCH("norm_fwd", (norm_fwd_kernel<E, N, P, kMaxPieces / P, LAYER>), dim3(blocks), dim3(threads), 0, st, a);
 }
