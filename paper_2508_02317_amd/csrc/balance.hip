@@ -14,10 +14,12 @@ namespace moe {
 
 namespace {
 
+constexpr int kPieces = 2;                             // of 16 bytes that a lane has of a row, if the row has more than 64 lanes' worth: as many as it takes
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr int kFwdThreads = 512, kFwdWaves = kFwdThreads / 64, kFwdBlocks = 256;
-constexpr int kBwdThreads = 256, kBwdBlocks = 4096;
+constexpr int kBwdThreads = 512, kBwdBlocks = 512;
 constexpr size_t kHeadBytes = 512;                     // of the workspace: the join's counter and losses
 constexpr int kJoinThreads = 1024, kJoinLanes = 32;    // lanes of a row of sums, at most
 
@@ -27,9 +29,9 @@ struct FwdArgs {
   const uint8_t* valid;                                // or null
   float *losses, *importance, *lse;
   int32_t* counts;
-  int T, E, k, lanes;
+  int T, E, k, lanes, row;                             // row: E rounded up to whole pieces
   Divisor per_token;                                   // k
-  // workspace: sums and counts [blocks][E], z and n [blocks], the join's losses and its counter
+  // workspace: sums and counts [blocks][row], z and n [blocks], the join's losses and its counter
   float *sum_of, *z_of;
   int32_t *count_of, *n_of;
   double* loss_of;
@@ -46,18 +48,40 @@ struct BwdArgs {
   float balance, z;
 };
 
-template <int N> __device__ __forceinline__ void load(float (&v)[N], const float* p) {
-  if constexpr (N == 4) {
-    const f32x4 x = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+// Four consecutive elements of a row from column e on, where the row has them.  Rows of E elements start at multiples of 4 bytes, which is all that a
+// 16-byte access needs.  (The logits have just been written by the router's product, the gradient goes to its backward product: loads pass through the caches.)
+// Loads are in straight-line code, at places that exist, and nothing touches what they bring before it is used: a load behind a branch, or one whose result
+// is masked at once, is waited for there, and nothing would be in flight from one turn to the next.
+// TAIL: E is no multiple of four.  A piece that would pass the row's end is read from the last four elements and moved into place when it is used.
+template <bool TAIL> __device__ __forceinline__ f32x4 fetch(const float* row, int e, int E) {
+  if (TAIL && E < 4) return f32x4{row[0], row[min(1, E - 1)], row[min(2, E - 1)], 0.0f};
+  return *reinterpret_cast<const f32x4_at_4*>(row + min(e, E - 4));
+}
+template <bool TAIL> __device__ __forceinline__ void place(float (&v)[4], const f32x4& x, int e, int E, float beyond) {
+  const int shift = TAIL && E < 4 ? e : e - min(e, E - 4);
+  if (TAIL) {
+    v[0] = shift == 0 ? x[0] : shift == 1 ? x[1] : shift == 2 ? x[2] : shift == 3 ? x[3] : beyond;
+    v[1] = shift == 0 ? x[1] : shift == 1 ? x[2] : shift == 2 ? x[3] : beyond;
+    v[2] = shift == 0 ? x[2] : shift == 1 ? x[3] : beyond;
+    v[3] = shift == 0 ? x[3] : beyond;
+    if (E < 4) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = x[q];
+      for (int q = 1; q < 4; ++q)
+        if (q >= E) v[q] = beyond;
+    }
   } else {
-    v[0] = *p;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = shift == 0 ? x[q] : beyond;
   }
 }
-template <int N> __device__ __forceinline__ void store(const float (&v)[N], float* p) {
-  if constexpr (N == 4) __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
-  else *p = v[0];
+template <bool TAIL> __device__ __forceinline__ void store(const float (&v)[4], float* row, int e, int E) {
+  if (!TAIL || e + 4 <= E) {
+    __builtin_nontemporal_store(f32x4_at_4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_at_4*>(row + e));
+  } else {
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+      if (e + q < E) row[e + q] = v[q];
+  }
 }
 
 __device__ __forceinline__ double block_sum(double v, double* scratch) {   // scratch: one of each wave; the result in thread 0
@@ -71,46 +95,43 @@ __device__ __forceinline__ double block_sum(double v, double* scratch) {   // sc
   return all;
 }
 
-// What becomes of an expert's sums; returns its part of the balance loss.
+// What becomes of an expert's sums; returns its part of sum_e c_e P_e.
 __device__ __forceinline__ double finish_expert(const FwdArgs& a, int e, float sum, int32_t count, int32_t n) {
-  const float many = static_cast<float>(max(n, 1)), importance = sum / many;
+  const float importance = sum / static_cast<float>(max(n, 1));
   a.importance[e] = importance;
   a.counts[e] = count;
-  return static_cast<double>(count) * a.E / (static_cast<double>(a.k) * max(n, 1)) * importance;
+  return static_cast<double>(count) * importance;
 }
 __device__ __forceinline__ void finish(const FwdArgs& a, double balance, double z, int32_t n) {
-  a.losses[0] = static_cast<float>(balance);
-  a.losses[1] = static_cast<float>(z / max(n, 1));
+  const double many = max(n, 1);
+  a.losses[0] = static_cast<float>(balance * a.E / (many * a.k));
+  a.losses[1] = static_cast<float>(z / many);
   a.counts[a.E] = n;
 }
 
-// N columns a piece (4 where rows are whole pieces of 16 bytes), P pieces a lane.  ONE: the only workgroup, which needs no join.
-template <int N, int P, bool ONE>
+// P pieces of four columns a lane.  ONE: the only workgroup, which needs no join.
+template <int P, bool TAIL, bool ONE>
 __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
-  extern __shared__ char shared[];                     // [waves][E] sums, [E] counts
+  extern __shared__ char shared[];                     // [waves][row] sums, [row] counts
   __shared__ double scratch[kFwdWaves];
   __shared__ float z_wave[kFwdWaves];
   __shared__ int n_wave[kFwdWaves];
   float* sums = reinterpret_cast<float*>(shared);
-  int32_t* counts = reinterpret_cast<int32_t*>(sums + kFwdWaves * a.E);
+  int32_t* counts = reinterpret_cast<int32_t*>(sums + kFwdWaves * a.row);
   const int l = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6, lane = l & (a.lanes - 1), group = static_cast<int>(threadIdx.x) / a.lanes;
   const int groups = kFwdThreads / a.lanes;
   const long step = static_cast<long>(gridDim.x) * groups;
   long t = static_cast<long>(blockIdx.x) * groups + group;
   // what is needed first is requested first: the rows of the first turn, this workgroup's share of the pairs, then the rows of each next turn
-  float v[P][N];
-  uint32_t on;
-  auto fetch = [&](long row) {
-    on = row < a.T ? a.valid ? a.valid[row] : 1u : 0u;
+  f32x4 x[P];
+  uint32_t on = 0;
+  auto request = [&](long row) {
+    const long r = min(row, a.T - 1l);
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int e = (p * a.lanes + lane) * N;
-#pragma unroll
-      for (int q = 0; q < N; ++q) v[p][q] = -INFINITY;
-      if (row < a.T && e < a.E) load(v[p], a.logits + row * a.E + e);
-    }
+    for (int p = 0; p < P; ++p) x[p] = fetch<TAIL>(a.logits + r * a.E, (p * a.lanes + lane) * 4, a.E);
+    on = a.valid ? a.valid[r] : 1u;
   };
-  fetch(t);
+  if (a.T > 0) request(t);
   for (int e = threadIdx.x; e < a.E; e += kFwdThreads) counts[e] = 0;
   {
     const long share = (a.T + static_cast<long>(gridDim.x) - 1) / gridDim.x, first = blockIdx.x * share * a.k, last = min(first + share * a.k, static_cast<long>(a.T) * a.k);
@@ -126,30 +147,32 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
       if (a.valid) counted = a.valid[divide(static_cast<uint32_t>(i), a.per_token)];
     }
   }
-  float acc[P][N], z_sum = 0.0f;
+  float acc[P][4], z_sum = 0.0f;
   int n = 0;
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int q = 0; q < N; ++q) acc[p][q] = 0.0f;
+    for (int q = 0; q < 4; ++q) acc[p][q] = 0.0f;
   for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += step, t += step) {
-    const bool there = on != 0;
-    float e[P][N], top = -INFINITY;
+    const bool there = t < a.T && on != 0;
+    float e[P][4], top = -INFINITY;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+      place<TAIL>(e[p], x[p], (p * a.lanes + lane) * 4, a.E, -INFINITY);
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
-        e[p][q] = there ? v[p][q] : -INFINITY;         // padding may hold anything
+      for (int q = 0; q < 4; ++q) {
+        if (!there) e[p][q] = -INFINITY;               // padding may hold anything
         top = fmaxf(top, e[p][q]);
       }
-    if (base + step < a.T) fetch(t + step);
+    }
+    request(t + step);
     top = lanes_max(top, a.lanes);
     const float from = top == -INFINITY ? 0.0f : top;  // a row without a finite logit has no probabilities
     float total = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
+      for (int q = 0; q < 4; ++q) {
         e[p][q] = expf(e[p][q] - from);
         total += e[p][q];
       }
@@ -158,7 +181,7 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < N; ++q) acc[p][q] += e[p][q] * scale;
+      for (int q = 0; q < 4; ++q) acc[p][q] += e[p][q] * scale;
     if (lane == 0 && t < a.T) {
       a.lse[t] = lse;
       n += there;
@@ -170,17 +193,17 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < N; ++q) acc[p][q] += __shfl_xor(acc[p][q], o, 64);
+      for (int q = 0; q < 4; ++q) acc[p][q] += __shfl_xor(acc[p][q], o, 64);
   }
   z_sum = wave_sum(z_sum);
   n = wave_sum_i(n);
   if (l < a.lanes) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int e = (p * a.lanes + lane) * N;
+      const int e = (p * a.lanes + lane) * 4;
       if (e < a.E) {
 #pragma unroll
-        for (int q = 0; q < N; ++q) sums[wave * a.E + e + q] = acc[p][q];
+        for (int q = 0; q < 4; ++q) sums[wave * a.row + e + q] = acc[p][q];
       }
     }
   }
@@ -192,12 +215,12 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
   double balance = 0.0;
   for (int e = threadIdx.x; e < a.E; e += kFwdThreads) {
     float sum = 0.0f;
-    for (int w = 0; w < kFwdWaves; ++w) sum += sums[w * a.E + e];
+    for (int w = 0; w < kFwdWaves; ++w) sum += sums[w * a.row + e];
     if (ONE) {
       balance += finish_expert(a, e, sum, counts[e], n);
     } else {
-      a.sum_of[static_cast<long>(blockIdx.x) * a.E + e] = sum;
-      a.count_of[static_cast<long>(blockIdx.x) * a.E + e] = counts[e];
+      a.sum_of[static_cast<long>(blockIdx.x) * a.row + e] = sum;
+      a.count_of[static_cast<long>(blockIdx.x) * a.row + e] = counts[e];
     }
   }
   if (ONE) {
@@ -210,59 +233,61 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
   }
 }
 
-// The workgroups' rows added: `lanes` (a power of two up to kJoinLanes) lanes of N experts a workgroup, the rows dealt out to kJoinThreads / lanes runs, which are
+// The workgroups' rows added: `lanes` (a power of two up to kJoinLanes) lanes of four experts a workgroup, the rows dealt out to kJoinThreads / lanes runs, which are
 // added over a wave and over the waves.  The last workgroup to end, by a counter that the launch before has cleared, adds the losses of all in the order of
 // their numbers.
-template <int N> __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, int parts, int lanes) {
+__global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, int parts, int lanes) {
   constexpr int kWaves = kJoinThreads / 64;
-  __shared__ float sums[kWaves][kJoinLanes * N];
-  __shared__ int32_t counts[kWaves][kJoinLanes * N], n_wave[kWaves];
-  __shared__ double scratch[2][kWaves];
+  __shared__ float sums[kWaves][kJoinLanes * 4];
+  __shared__ int32_t counts[kWaves][kJoinLanes * 4], n_all;
+  __shared__ double scratch[kWaves], z_all;
   const int l = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6, lane = l & (lanes - 1), runs = kJoinThreads / lanes;
-  const int e = (blockIdx.x * lanes + lane) * N;
-  float sum[N] = {};
-  int32_t count[N] = {};
-  if (e < a.E) {
-#pragma unroll 4
-    for (int i = static_cast<int>(threadIdx.x) / lanes; i < parts; i += runs) {
-      const long at = static_cast<long>(i) * a.E + e;
-      if constexpr (N == 4) {
-        const f32x4 s = *reinterpret_cast<const f32x4*>(a.sum_of + at);
-        const i32x4 c = *reinterpret_cast<const i32x4*>(a.count_of + at);
-#pragma unroll
-        for (int q = 0; q < N; ++q) { sum[q] += s[q]; count[q] += c[q]; }
-      } else {
-        sum[0] += a.sum_of[at];
-        count[0] += a.count_of[at];
-      }
-    }
-  }
+  const int e = (blockIdx.x * lanes + lane) * 4;
+  f32x4 sum = {};
+  i32x4 count = {};
   int n = 0;
   double z = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kJoinThreads) { n += a.n_of[i]; z += a.z_of[i]; }
+  if (wave == kWaves - 1) {                            // tokens and squares are the last wave's to sum, beside its columns
+#pragma unroll
+    for (int u = 0; u < kFwdBlocks / 64; ++u) {
+      const int i = u * 64 + l;
+      n += i < parts ? a.n_of[i] : 0;
+      z += i < parts ? a.z_of[i] : 0.0f;
+    }
+  }
+  if (e < a.E) {
+#pragma unroll 8
+    for (int i = static_cast<int>(threadIdx.x) / lanes; i < parts; i += runs) {
+      const long at = static_cast<long>(i) * a.row + e;
+      sum += *reinterpret_cast<const f32x4*>(a.sum_of + at);
+      count += *reinterpret_cast<const i32x4*>(a.count_of + at);   // behind E, in a row's last piece, lies anything
+    }
+  }
+  if (wave == kWaves - 1) {
+    n = wave_sum_i(n);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
+    if (l == 0) { n_all = n; z_all = z; }
+  }
   for (int o = lanes; o < 64; o *= 2)
 #pragma unroll
-    for (int q = 0; q < N; ++q) { sum[q] += __shfl_xor(sum[q], o, 64); count[q] += __shfl_xor(count[q], o, 64); }
+    for (int q = 0; q < 4; ++q) { sum[q] += __shfl_xor(sum[q], o, 64); count[q] += __shfl_xor(count[q], o, 64); }
   if (l < lanes) {
 #pragma unroll
-    for (int q = 0; q < N; ++q) { sums[wave][lane * N + q] = sum[q]; counts[wave][lane * N + q] = count[q]; }
+    for (int q = 0; q < 4; ++q) { sums[wave][lane * 4 + q] = sum[q]; counts[wave][lane * 4 + q] = count[q]; }
   }
-  n = wave_sum_i(n);
-  if (l == 0) n_wave[wave] = n;
-  z = block_sum(z, scratch[0]);                        // its barrier stands before the reads below too
-  n = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) n += n_wave[w];
+  __syncthreads();
+  n = n_all;
   double balance = 0.0;
-  const int mine = blockIdx.x * lanes * N + threadIdx.x;
-  if (static_cast<int>(threadIdx.x) < lanes * N && mine < a.E) {
+  const int mine = blockIdx.x * lanes * 4 + threadIdx.x;
+  if (static_cast<int>(threadIdx.x) < lanes * 4 && mine < a.E) {
     float s = 0.0f;
     int32_t c = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) { s += sums[w][threadIdx.x]; c += counts[w][threadIdx.x]; }
     balance = finish_expert(a, mine, s, c, n);
   }
-  balance = block_sum(balance, scratch[1]);
+  balance = block_sum(balance, scratch);
   if (threadIdx.x != 0) return;
   if (gridDim.x > 1) {
     __hip_atomic_store(&a.loss_of[blockIdx.x], balance, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -270,84 +295,82 @@ template <int N> __global__ __launch_bounds__(kJoinThreads) void balance_join_ke
     balance = 0.0;
     for (unsigned i = 0; i < gridDim.x; ++i) balance += __hip_atomic_load(&a.loss_of[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  finish(a, balance, z, n);
+  finish(a, balance, z_all, n);
 }
 
-template <int N, int P>
+template <int P, bool TAIL, bool ADD>
 __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
   const int lane = static_cast<int>(threadIdx.x) & (a.lanes - 1), group = static_cast<int>(threadIdx.x) / a.lanes, groups = kBwdThreads / a.lanes;
   const long step = static_cast<long>(gridDim.x) * groups;
   long t = static_cast<long>(blockIdx.x) * groups + group;
-  float v[P][N], more[P][N], lse;
+  f32x4 x[P], more[P];
+  float lse_next;
   uint32_t on;
-  auto fetch = [&](long row) {
-    const bool inside = row < a.T;
-    on = inside ? a.valid ? a.valid[row] : 1u : 0u;
-    lse = inside ? a.lse[row] : 0.0f;
+  auto request = [&](long row) {
+    const long r = min(row, a.T - 1l);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int e = (p * a.lanes + lane) * N;
-#pragma unroll
-      for (int q = 0; q < N; ++q) { v[p][q] = -INFINITY; more[p][q] = 0.0f; }
-      if (inside && e < a.E) {
-        load(v[p], a.logits + row * a.E + e);
-        if (a.add) load(more[p], a.add + row * a.E + e);
-      }
+      const int e = (p * a.lanes + lane) * 4;
+      x[p] = fetch<TAIL>(a.logits + r * a.E, e, a.E);
+      if constexpr (ADD) more[p] = fetch<TAIL>(a.add + r * a.E, e, a.E);
     }
+    lse_next = a.lse[r];
+    on = a.valid ? a.valid[r] : 1u;
   };
-  fetch(t);
+  request(t);
+  float share[P][4];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int e = (p * a.lanes + lane) * 4 + q, count = a.counts[min(e, a.E)];
+      share[p][q] = e < a.E ? static_cast<float>(count) : 0.0f;
+    }
   const float many = static_cast<float>(max(a.counts[a.E], 1));
   const float to_balance = a.balance * (a.dlosses ? a.dlosses[0] : 1.0f) / many, to_z = 2.0f * a.z * (a.dlosses ? a.dlosses[1] : 1.0f) / many;
   const float per_pair = static_cast<float>(a.E) / static_cast<float>(a.k) / many;
-  float share[P][N];
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int e = (p * a.lanes + lane) * N;
+  for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int q = 0; q < N; ++q) share[p][q] = 0.0f;
-    if (e < a.E) {
-      if constexpr (N == 4) {
-        const i32x4 c = *reinterpret_cast<const i32x4*>(a.counts + e);
-#pragma unroll
-        for (int q = 0; q < N; ++q) share[p][q] = static_cast<float>(c[q]) * per_pair;
-      } else {
-        share[p][0] = static_cast<float>(a.counts[e]) * per_pair;
-      }
-    }
-  }
+    for (int q = 0; q < 4; ++q) share[p][q] *= per_pair;
   for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += step, t += step) {
+    const float lse = lse_next;
     const bool any = on != 0 && lse != -INFINITY;      // else the token does not count, or has no finite logit
     const float level = any ? lse * to_z : 0.0f;
-    float e[P][N], out[P][N], sums[2] = {0.0f, 0.0f};
+    float e[P][4], out[P][4], sums[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * a.lanes + lane) * 4;
+      place<TAIL>(e[p], x[p], c, a.E, -INFINITY);
+      if constexpr (ADD) place<TAIL>(out[p], more[p], c, a.E, 0.0f);
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
-        e[p][q] = any ? expf(v[p][q] - lse) : 0.0f;
-        out[p][q] = more[p][q];
+      for (int q = 0; q < 4; ++q) {
+        e[p][q] = any ? expf(e[p][q] - lse) : 0.0f;
+        if constexpr (!ADD) out[p][q] = 0.0f;
         sums[0] += e[p][q];
         sums[1] += share[p][q] * e[p][q];
       }
-    if (base + step < a.T) fetch(t + step);
+    }
+    request(t + step);
     // the sum of exp(z - lse) is 1 but for the rounding of lse, which dividing by it takes out of the probabilities
     const float total = lanes_sum(sums[0], a.lanes), scale = total == 0.0f ? 0.0f : 1.0f / total, mean = lanes_sum(sums[1], a.lanes) * scale;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c = (p * a.lanes + lane) * N;
+      const int c = (p * a.lanes + lane) * 4;
 #pragma unroll
-      for (int q = 0; q < N; ++q) out[p][q] += e[p][q] * scale * ((share[p][q] - mean) * to_balance + level);
-      if (t < a.T && c < a.E) store(out[p], a.dlogits + t * a.E + c);
+      for (int q = 0; q < 4; ++q) out[p][q] += e[p][q] * scale * ((share[p][q] - mean) * to_balance + level);
+      if (t < a.T && c < a.E) store<TAIL>(out[p], a.dlogits + t * a.E, c, a.E);
     }
   }
 }
 
-// How the E columns of a row are dealt out: four pieces a lane where the row has as many
-struct Split { int width, lanes, pieces; };
+// How the E columns of a row are dealt out: kPieces pieces a lane where the row has as many
+struct Split { int row, lanes, pieces; };
 Split split_columns(int E) {
-  Split s{E % 4 == 0 ? 4 : 1, 1, 1};
-  const int pieces = E / s.width;
-  while (s.lanes < 64 && s.lanes * 4 < pieces) s.lanes *= 2;
-  while (s.lanes * s.pieces < pieces) s.pieces *= 2;
+  const int all = ceil_div(E, 4);
+  Split s{4 * all, 1, 1};
+  while (s.lanes < 64 && s.lanes * kPieces < all) s.lanes *= 2;
+  while (s.lanes * s.pieces < all) s.pieces *= 2;
   return s;
 }
 int fwd_blocks(int T, int E) {
@@ -364,16 +387,11 @@ int32_t check_balance(const char* who, int T, int E, int k) {
   return MOE_OK;
 }
 
-template <class F> void with_split(const Split& s, F f) {
-  using std::integral_constant;
-  if (s.width == 4) {
-    if (s.pieces == 1) f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (s.pieces == 2) f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    else f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-  } else {
-    if (s.pieces <= 4) f(integral_constant<int, 1>{}, integral_constant<int, 4>{});
-    else f(integral_constant<int, 1>{}, integral_constant<int, 16>{});
-  }
+template <class F> void with_pieces(int pieces, bool tail, F f) {
+  auto tailed = [&](auto p) { if (tail) f(p, std::true_type{}); else f(p, std::false_type{}); };
+  if (pieces == 1) tailed(std::integral_constant<int, 1>{});
+  else if (pieces == 2) tailed(std::integral_constant<int, 2>{});
+  else tailed(std::integral_constant<int, 4>{});       // 64 lanes of up to 1024 experts
 }
 
 }  // namespace
@@ -386,7 +404,7 @@ extern "C" size_t moe_balance_loss_fwd_workspace_bytes(int T, int E, int k) {
   (void)k;
   if (T < 0 || E <= 0 || E > kMaxExperts) return 0;
   const size_t blocks = fwd_blocks(T, E);
-  return align_up(blocks * (2 * static_cast<size_t>(E) + 2) * 4, 16) + kHeadBytes;
+  return align_up(blocks * (2 * static_cast<size_t>(split_columns(E).row) + 2) * 4, 16) + kHeadBytes;
 }
 
 extern "C" int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int E, int k, float* losses, int32_t* counts,
@@ -399,28 +417,28 @@ extern "C" int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk
   MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "balance_loss_fwd: workspace null, misaligned or smaller than %zu bytes", need);
   const Split s = split_columns(E);
   const int blocks = fwd_blocks(T, E);
-  FwdArgs a{logits, topk_idx, valid, losses, importance, lse, counts, T, E, k, s.lanes, divisor(k), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+  FwdArgs a{logits, topk_idx, valid, losses, importance, lse, counts, T, E, k, s.lanes, s.row, divisor(k), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   a.joined = static_cast<uint32_t*>(ws);
   a.loss_of = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);                 // of the join's workgroups
   static_assert(16 + kMaxExperts / kJoinLanes * sizeof(double) <= kHeadBytes);
   a.sum_of = reinterpret_cast<float*>(static_cast<char*>(ws) + kHeadBytes);
-  a.count_of = reinterpret_cast<int32_t*>(a.sum_of + static_cast<size_t>(blocks) * E);
-  a.z_of = reinterpret_cast<float*>(a.count_of + static_cast<size_t>(blocks) * E);
+  a.count_of = reinterpret_cast<int32_t*>(a.sum_of + static_cast<size_t>(blocks) * s.row);
+  a.z_of = reinterpret_cast<float*>(a.count_of + static_cast<size_t>(blocks) * s.row);
   a.n_of = reinterpret_cast<int32_t*>(a.z_of + blocks);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const size_t lds = (kFwdWaves + 1) * static_cast<size_t>(E) * 4;
+  const size_t lds = (kFwdWaves + 1) * static_cast<size_t>(s.row) * 4;
   begin_call("moe_balance_loss_fwd", st);
-  with_split(s, [&](auto n, auto p) {
-    constexpr int N = decltype(n)::value, P = decltype(p)::value;
-    if (blocks == 1) MOE_LAUNCH("balance_fwd", (balance_fwd_kernel<N, P, true>), dim3(1), dim3(kFwdThreads), lds, st, a);
-    else MOE_LAUNCH("balance_fwd", (balance_fwd_kernel<N, P, false>), dim3(blocks), dim3(kFwdThreads), lds, st, a);
+  with_pieces(s.pieces, E % 4 != 0, [&](auto p, auto t) {
+    constexpr int P = decltype(p)::value;
+    constexpr bool TAIL = decltype(t)::value;
+    if (blocks == 1) MOE_LAUNCH("balance_fwd", (balance_fwd_kernel<P, TAIL, true>), dim3(1), dim3(kFwdThreads), lds, st, a);
+    else MOE_LAUNCH("balance_fwd", (balance_fwd_kernel<P, TAIL, false>), dim3(blocks), dim3(kFwdThreads), lds, st, a);
   });
   if (blocks > 1) {
-    const int pieces = E / s.width;
+    const int pieces = s.row / 4;
     int lanes = 1;
     while (lanes < pieces && lanes < kJoinLanes) lanes *= 2;
-    if (s.width == 4) MOE_LAUNCH("balance_join", balance_join_kernel<4>, dim3(ceil_div(pieces, lanes)), dim3(kJoinThreads), 0, st, a, blocks, lanes);
-    else MOE_LAUNCH("balance_join", balance_join_kernel<1>, dim3(ceil_div(pieces, lanes)), dim3(kJoinThreads), 0, st, a, blocks, lanes);
+    MOE_LAUNCH("balance_join", balance_join_kernel, dim3(ceil_div(pieces, lanes)), dim3(kJoinThreads), 0, st, a, blocks, lanes);
   }
   return end_call();
 }
@@ -437,9 +455,12 @@ extern "C" int32_t moe_balance_loss_bwd(const float* logits, const int32_t* coun
   const int rows = kBwdThreads / s.lanes, blocks = T / rows + (T % rows != 0);
   hipStream_t st = static_cast<hipStream_t>(stream);
   begin_call("moe_balance_loss_bwd", st);
-  with_split(s, [&](auto n, auto p) {
-    constexpr int N = decltype(n)::value, P = decltype(p)::value;
-    MOE_LAUNCH("balance_bwd", (balance_bwd_kernel<N, P>), dim3(blocks < kBwdBlocks ? blocks : kBwdBlocks), dim3(kBwdThreads), 0, st, a);
+  with_pieces(s.pieces, E % 4 != 0, [&](auto p, auto t) {
+    constexpr int P = decltype(p)::value;
+    constexpr bool TAIL = decltype(t)::value;
+    const dim3 grid(blocks < kBwdBlocks ? blocks : kBwdBlocks);
+    if (add) MOE_LAUNCH("balance_bwd", (balance_bwd_kernel<P, TAIL, true>), grid, dim3(kBwdThreads), 0, st, a);
+    else MOE_LAUNCH("balance_bwd", (balance_bwd_kernel<P, TAIL, false>), grid, dim3(kBwdThreads), 0, st, a);
   });
   return end_call();
 }
