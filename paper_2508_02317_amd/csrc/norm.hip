@@ -16,8 +16,8 @@ namespace moe {
 namespace {
 
 constexpr int kMaxDim = 16384;
-constexpr int kMaxPieces = 4;                          // 16-byte pieces of a row that one lane holds
-constexpr int kFwdThreads = 256, kBwdThreads = 512;    // at least; a row of more waves has a workgroup of them
+constexpr int kFwdPieces = 4, kBwdPieces = 2;          // 16-byte pieces of a row that one lane holds; of shorter rows, several at once
+constexpr int kFwdThreads = 256, kBwdThreads = 512, kMaxThreads = 1024;   // at least; a row of more waves has a workgroup of them
 constexpr int kFwdBlocks = 2048, kBwdBlocks = 256;     // at most
 constexpr int kJoinColumns = 64, kJoinThreads = 1024;
 
@@ -92,54 +92,52 @@ template <int K> struct Sums {
   }
 };
 
-// P pieces of N elements a lane, U rows at once
-template <class E, int N, int P, int U, bool LAYER>
-__global__ __launch_bounds__(1024) void norm_fwd_kernel(NormArgs a) {
+// P pieces of N elements a lane, U rows at once.  Loads are in straight-line code, at places that exist: one behind a branch is waited for where the paths meet.
+template <class E, int N, int P, int U, bool LAYER, bool SUM>
+__global__ __launch_bounds__(sizeof(E) == 2 ? kMaxThreads / 2 : kMaxThreads) void norm_fwd_kernel(NormArgs a) {
   __shared__ Sums<U> sums;
   const Place me(a.lanes, a.waves);
   int turn = 0;
+  const long step = static_cast<long>(me.groups) * U, all = step * gridDim.x;
+  Piece<E, N> x[U][P], res[U][P];
+  uint32_t t[U], h[U];
+  auto request = [&](long base) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t row = static_cast<uint32_t>(min(base + u * me.groups + me.group, a.rows - 1l));
+      t[u] = divide(row, a.per_token);
+      h[u] = row - t[u] * a.heads;
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int column = min((p * me.size + me.lane) * N, a.dim - N);
+        x[u][p].load(at<const E>(a.x, t[u], h[u]) + column);
+        if constexpr (SUM) res[u][p].load(at<const E>(a.residual, t[u], h[u]) + column);
+      }
+    }
+  };
+  request(static_cast<long>(blockIdx.x) * step);
   float w[P][N], b[P][N];
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int column = (p * me.size + me.lane) * N;
+    const int column = min((p * me.size + me.lane) * N, a.dim - N);
 #pragma unroll
     for (int q = 0; q < N; ++q) { w[p][q] = 1.0f; b[p][q] = 0.0f; }
-    if (column < a.dim && a.weight) weights(w[p], a.weight, a.weight_bf16, column);
-    if (column < a.dim && a.bias) weights(b[p], a.bias, a.weight_bf16, column);
+    if (a.weight) weights(w[p], a.weight, a.weight_bf16, column);
+    if (a.bias) weights(b[p], a.bias, a.weight_bf16, column);
   }
-  const int step = me.groups * U;
-  for (long base = static_cast<long>(blockIdx.x) * step; base < a.rows; base += static_cast<long>(gridDim.x) * step) {
-    Piece<E, N> x[U][P], res[U][P];
-    uint32_t t[U], h[U];
+  for (long base = static_cast<long>(blockIdx.x) * step; base < a.rows; base += all) {
     bool there[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long row = base + u * me.groups + me.group;
-      there[u] = row < a.rows;
-      t[u] = there[u] ? divide(static_cast<uint32_t>(row), a.per_token) : 0;
-      h[u] = there[u] ? static_cast<uint32_t>(row) - t[u] * a.heads : 0;
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int column = (p * me.size + me.lane) * N;
-        const float zero[N] = {};
-        x[u][p].set(zero);
-        res[u][p].set(zero);
-        if (there[u] && column < a.dim) {
-          x[u][p].load(at<const E>(a.x, t[u], h[u]) + column);
-          if (a.residual.p) res[u][p].load(at<const E>(a.residual, t[u], h[u]) + column);
-        }
-      }
-    }
     float v[U][P][N], total[U], mean[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      there[u] = base + u * me.groups + me.group < a.rows;
       total[u] = 0.0f;
       mean[u] = 0.0f;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int column = (p * me.size + me.lane) * N;
         x[u][p].get(v[u][p]);
-        if (a.residual.p) {
+        if constexpr (SUM) {
           float r[N];
           res[u][p].get(r);
 #pragma unroll
@@ -148,10 +146,16 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormArgs a) {
           x[u][p].get(v[u][p]);
           if (there[u] && column < a.dim) x[u][p].store(at<E>(a.sum, t[u], h[u]) + column);
         }
+        if (column < a.dim) {
 #pragma unroll
-        for (int q = 0; q < N; ++q) total[u] += LAYER ? v[u][p][q] : v[u][p][q] * v[u][p][q];
+          for (int q = 0; q < N; ++q) total[u] += LAYER ? v[u][p][q] : v[u][p][q] * v[u][p][q];
+        }
       }
     }
+    uint32_t tt[U], hh[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { tt[u] = t[u]; hh[u] = h[u]; }
+    if (base + all < a.rows) request(base + all);
     sums(total, a.lanes, a.waves, me.wave, turn);
     if (LAYER) {
 #pragma unroll
@@ -189,14 +193,14 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormArgs a) {
         for (int q = 0; q < N; ++q) y[q] = v[u][p][q] * rstd * w[p][q] + b[p][q];
         Piece<E, N> o;
         o.set(y);
-        o.store(at<E>(a.y, t[u], h[u]) + column);
+        o.store(at<E>(a.y, tt[u], hh[u]) + column);
       }
     }
   }
 }
 
-template <class E, int N, int P, int U, bool LAYER>
-__global__ __launch_bounds__(sizeof(E) == 4 ? 1024 : 512) void norm_bwd_kernel(NormArgs a) {
+template <class E, int N, int P, int U, bool LAYER, bool WITH_DB, bool ADD, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a) {
   constexpr int K = LAYER ? 2 : 1;
   __shared__ Sums<U * K> sums;
   extern __shared__ __align__(16) float columns[];     // [half of the waves, or sets of them][D] of dw, then of db: 32 KiB at most
@@ -210,55 +214,63 @@ __global__ __launch_bounds__(sizeof(E) == 4 ? 1024 : 512) void norm_bwd_kernel(N
     for (int q = 0; q < N; ++q) { w[p][q] = 1.0f; dw[p][q] = 0.0f; db[p][q] = 0.0f; }
     if (column < a.dim && a.weight) weights(w[p], a.weight, a.weight_bf16, column);
   }
-  const int step = me.groups * U;
-  for (long base = static_cast<long>(blockIdx.x) * step; base < a.rows; base += static_cast<long>(gridDim.x) * step) {
-    Piece<E, N> x[U][P], dy[U][P], add[U][P];
-    uint32_t t[U], h[U];
-    bool there[U];
-    float mean[U], rstd[U];
+  const long step = static_cast<long>(me.groups) * U, all = step * gridDim.x;
+  // The next rows are requested when the present ones have been taken: loads in straight-line code, at places that exist, untouched until they are used (a
+  // load behind a branch, or one that is masked at once, is waited for there).
+  Piece<E, N> x[U][P], dy[U][P], add[U][P];
+  uint32_t t[U], h[U];
+  float mean_of[U], rstd_of[U];
+  auto request = [&](long base) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long row = base + u * me.groups + me.group;
-      there[u] = row < a.rows;
-      t[u] = there[u] ? divide(static_cast<uint32_t>(row), a.per_token) : 0;
-      h[u] = there[u] ? static_cast<uint32_t>(row) - t[u] * a.heads : 0;
-      rstd[u] = there[u] ? a.rstd[row] : 0.0f;
-      mean[u] = LAYER && there[u] ? a.mean[row] : 0.0f;
+      const uint32_t row = static_cast<uint32_t>(min(base + u * me.groups + me.group, a.rows - 1l));
+      t[u] = divide(row, a.per_token);
+      h[u] = row - t[u] * a.heads;
+      rstd_of[u] = a.rstd[row];
+      if constexpr (LAYER) mean_of[u] = a.mean[row];
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const int column = (p * me.size + me.lane) * N;
-        const float zero[N] = {};
-        x[u][p].set(zero);
-        dy[u][p].set(zero);
-        add[u][p].set(zero);
-        if (there[u] && column < a.dim) {
-          x[u][p].load(at<const E>(a.x, t[u], h[u]) + column);
-          dy[u][p].load(at<const E>(a.dy, t[u], h[u]) + column);
-          if (a.add.p) add[u][p].load(at<const E>(a.add, t[u], h[u]) + column);
-        }
+        const int column = min((p * me.size + me.lane) * N, a.dim - N);
+        x[u][p].load(at<const E>(a.x, t[u], h[u]) + column);
+        dy[u][p].load(at<const E>(a.dy, t[u], h[u]) + column);
+        if constexpr (ADD) add[u][p].load(at<const E>(a.add, t[u], h[u]) + column);
       }
     }
-    float xh[U][P][N], g[U][P][N], total[U * K];
+  };
+  request(static_cast<long>(blockIdx.x) * step);
+  for (long base = static_cast<long>(blockIdx.x) * step; base < a.rows; base += all) {
+    float xh[U][P][N], g[U][P][N], total[U * K], rstd[U], mean[U];
+    Piece<E, N> more[U][P];
+    E* to[U];
+    bool there[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      there[u] = base + u * me.groups + me.group < a.rows;
+      to[u] = at<E>(a.dx, t[u], h[u]);
+      rstd[u] = rstd_of[u];
+      if constexpr (LAYER) mean[u] = mean_of[u];
 #pragma unroll
       for (int k = 0; k < K; ++k) total[u * K + k] = 0.0f;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        float d[N];
-        x[u][p].get(xh[u][p]);
+        const bool real = there[u] && (p * me.size + me.lane) * N < a.dim;
+        float d[N], v[N];
+        x[u][p].get(v);
         dy[u][p].get(d);
+        if constexpr (ADD) more[u][p] = add[u][p];
 #pragma unroll
         for (int q = 0; q < N; ++q) {
-          xh[u][p][q] = (xh[u][p][q] - mean[u]) * rstd[u];
-          dw[p][q] += d[q] * xh[u][p][q];
-          db[p][q] += d[q];
+          d[q] = real ? d[q] : 0.0f;
+          xh[u][p][q] = real ? (LAYER ? v[q] - mean[u] : v[q]) * rstd[u] : 0.0f;
           g[u][p][q] = d[q] * w[p][q];
+          dw[p][q] += d[q] * xh[u][p][q];
+          if constexpr (WITH_DB) db[p][q] += d[q];
           total[u * K] += g[u][p][q] * xh[u][p][q];
           if (LAYER) total[u * K + K - 1] += g[u][p][q];
         }
       }
     }
+    request(base + all);
     sums(total, a.lanes, a.waves, me.wave, turn);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -268,13 +280,16 @@ __global__ __launch_bounds__(sizeof(E) == 4 ? 1024 : 512) void norm_bwd_kernel(N
       for (int p = 0; p < P; ++p) {
         const int column = (p * me.size + me.lane) * N;
         if (column >= a.dim) continue;
-        float o[N], more[N];
-        add[u][p].get(more);
+        float o[N];
+        if constexpr (ADD) more[u][p].get(o);
 #pragma unroll
-        for (int q = 0; q < N; ++q) o[q] = (g[u][p][q] - level - xh[u][p][q] * along) * rstd[u] + more[q];
+        for (int q = 0; q < N; ++q) {
+          const float own = (g[u][p][q] - level - xh[u][p][q] * along) * rstd[u];
+          o[q] = ADD ? own + o[q] : own;
+        }
         Piece<E, N> out;
         out.set(o);
-        out.store(at<E>(a.dx, t[u], h[u]) + column);
+        out.store(to[u] + column);
       }
     }
   }
@@ -354,43 +369,67 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float* pa
 
 // How rows of D elements are dealt out to lanes.
 struct Split { int lanes, waves, pieces; };
-Split split_row(int dtype, int D) {
+Split split_row(int dtype, int D, int most) {
   const int pieces = D / (16 / elem_size(dtype));
   Split s{1, 1, 1};
   while (s.lanes < 64 && s.lanes < pieces) s.lanes *= 2;
-  while (s.waves * 64 * kMaxPieces < pieces) s.waves *= 2;
+  while (s.waves * 64 * most < pieces && s.waves * 64 < kMaxThreads) s.waves *= 2;
   while (s.lanes * s.waves * s.pieces < pieces) s.pieces *= 2;
   return s;
 }
+constexpr int rows_at_once(int pieces, int most) { return pieces < most ? most / pieces : 1; }
 int threads_of(const Split& s, int least) { return s.waves * 64 > least ? s.waves * 64 : least; }
 int groups_of(const Split& s, int threads) { return s.waves > 1 ? threads / 64 / s.waves : threads / s.lanes; }
-int blocks_of(int rows, const Split& s, int threads, int most) {
-  const int step = groups_of(s, threads) * (kMaxPieces / s.pieces), n = rows / step + (rows % step != 0);
+int blocks_of(int rows, const Split& s, int threads, int pieces, int most) {
+  const int step = groups_of(s, threads) * rows_at_once(s.pieces, pieces), n = rows / step + (rows % step != 0);
   return n < most ? n : most;
 }
 
-template <bool BACK, class E, int N, int P, bool LAYER> void launch_norm(const NormArgs& a, int blocks, int threads, hipStream_t st) {
-  if constexpr (BACK)
-    MOE_LAUNCH("norm_bwd", (norm_bwd_kernel<E, N, P, kMaxPieces / P, LAYER>), dim3(blocks), dim3(threads), (a.want_dw || a.want_db) && threads / 64 > a.waves ? threads / 64 / a.waves / 2 * a.dim * 4 : 0, st, a);
-  else
-    MOE_LAUNCH("norm_fwd", (norm_fwd_kernel<E, N, P, kMaxPieces / P, LAYER>), dim3(blocks), dim3(threads), 0, st, a);
-}
-template <bool BACK> void launch_norm(const NormArgs& a, const Split& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
+// f(element type, elements of a piece, pieces of a lane) of a split
+template <class F> void with_split(const Split& s, int dtype, F f) {
+  using std::integral_constant;
   auto typed = [&](auto e, auto n) {
-    typedef decltype(e) E;
-    constexpr int N = decltype(n)::value;
-    if (layer) {
-      if (s.pieces == 1) launch_norm<BACK, E, N, 1, true>(a, blocks, threads, st);
-      else if (s.pieces == 2) launch_norm<BACK, E, N, 2, true>(a, blocks, threads, st);
-      else launch_norm<BACK, E, N, 4, true>(a, blocks, threads, st);
-    } else {
-      if (s.pieces == 1) launch_norm<BACK, E, N, 1, false>(a, blocks, threads, st);
-      else if (s.pieces == 2) launch_norm<BACK, E, N, 2, false>(a, blocks, threads, st);
-      else launch_norm<BACK, E, N, 4, false>(a, blocks, threads, st);
-    }
+    if (s.pieces == 1) f(e, n, integral_constant<int, 1>{});
+    else if (s.pieces == 2) f(e, n, integral_constant<int, 2>{});
+    else f(e, n, integral_constant<int, 4>{});
   };
-  if (dtype == MOE_BF16) typed(bf16_t{}, std::integral_constant<int, 8>{});
-  else typed(float{}, std::integral_constant<int, 4>{});
+  if (dtype == MOE_BF16) typed(bf16_t{}, integral_constant<int, 8>{});
+  else typed(float{}, integral_constant<int, 4>{});
+}
+void launch_fwd(const NormArgs& a, const Split& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
+  with_split(s, dtype, [&](auto e, auto n, auto p) {
+    auto launch = [&](auto kind, auto with_sum) {
+      typedef decltype(e) E;
+      constexpr int N = decltype(n)::value, P = decltype(p)::value, U = rows_at_once(P, kFwdPieces);
+      MOE_LAUNCH("norm_fwd", (norm_fwd_kernel<E, N, P, U, decltype(kind)::value, decltype(with_sum)::value>), dim3(blocks), dim3(threads), 0, st, a);
+    };
+    auto kinds = [&](auto with_sum) { if (layer) launch(std::true_type{}, with_sum); else launch(std::false_type{}, with_sum); };
+    if (a.residual.p) kinds(std::true_type{}); else kinds(std::false_type{});
+  });
+}
+void launch_bwd(const NormArgs& a, const Split& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
+  const int units = threads / 64 / a.waves;
+  const size_t lds = (a.want_dw || a.want_db) && units > 1 ? static_cast<size_t>(units / 2) * a.dim * 4 : 0;
+  with_split(s, dtype, [&](auto e, auto n, auto p) {
+    auto launch = [&](auto kind, auto add) {
+      typedef decltype(e) E;
+      constexpr int N = decltype(n)::value, P = decltype(p)::value, U = rows_at_once(P, kBwdPieces), KIND = decltype(kind)::value;
+      constexpr bool LAYER = KIND == 2, DB = KIND > 0, ADD = decltype(add)::value;
+      if constexpr (P == kBwdPieces || (P > kBwdPieces && sizeof(E) == 4)) {
+        if (threads > kBwdThreads) {                   // more than 8192 elements (bf16; 4096 in fp32)
+          MOE_LAUNCH("norm_bwd", (norm_bwd_kernel<E, N, P, U, LAYER, DB, ADD, kMaxThreads>), dim3(blocks), dim3(threads), lds, st, a);
+          return;
+        }
+      }
+      if constexpr (P <= kBwdPieces) MOE_LAUNCH("norm_bwd", (norm_bwd_kernel<E, N, P, U, LAYER, DB, ADD, kBwdThreads>), dim3(blocks), dim3(threads), lds, st, a);
+    };
+    auto kinds = [&](auto add) {                       // a layer norm's bias has its sums beside the weight's, wanted or not
+      if (layer) launch(std::integral_constant<int, 2>{}, add);
+      else if (a.want_db) launch(std::integral_constant<int, 1>{}, add);
+      else launch(std::integral_constant<int, 0>{}, add);
+    };
+    if (a.add.p) kinds(std::true_type{}); else kinds(std::false_type{});
+  });
 }
 
 int32_t check_norm(const char* who, int dtype, int weight_dtype, int T, int H, int D) {
@@ -425,13 +464,13 @@ extern "C" int32_t moe_norm_fwd(const void* x, int64_t x_stride_t, int64_t x_str
   a.x = rows(x, x_stride_t, x_stride_h); a.residual = rows(residual, r_stride_t, r_stride_h); a.sum = rows(sum, s_stride_t, s_stride_h); a.y = rows(y, y_stride_t, y_stride_h);
   MOE_REQUIRE(rows_ok(dtype, a.x) && rows_ok(dtype, a.y) && (!residual || (rows_ok(dtype, a.residual) && rows_ok(dtype, a.sum))) && aligned16(weight) && aligned16(bias),
               MOE_ERR_INVALID_ARG, "norm_fwd: tensors must be 16-byte aligned and strides multiples of 16 bytes");
-  const Split s = split_row(dtype, D);
+  const Split s = split_row(dtype, D, kFwdPieces);
   const int threads = threads_of(s, kFwdThreads);
   a.weight = weight; a.bias = bias; a.weight_bf16 = weight_dtype == MOE_BF16; a.mean = mean; a.rstd = rstd; a.rows = T * H; a.heads = H; a.dim = D;
   a.lanes = s.lanes; a.waves = s.waves; a.per_token = divisor(H); a.eps = eps; a.per_dim = 1.0f / static_cast<float>(D);
   hipStream_t st = static_cast<hipStream_t>(stream);
   begin_call("moe_norm_fwd", st);
-  launch_norm<false>(a, s, dtype, !rms, blocks_of(a.rows, s, threads, kFwdBlocks), threads, st);
+  launch_fwd(a, s, dtype, !rms, blocks_of(a.rows, s, threads, kFwdPieces, kFwdBlocks), threads, st);
   return end_call();
 }
 
@@ -455,14 +494,14 @@ extern "C" int32_t moe_norm_bwd(const void* dy, int64_t dy_stride_t, int64_t dy_
               aligned16(dbias), MOE_ERR_INVALID_ARG, "norm_bwd: tensors must be 16-byte aligned and strides multiples of 16 bytes");
   const size_t need = moe_norm_bwd_workspace_bytes(T, H, D);
   MOE_REQUIRE(!wanted || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE, "norm_bwd: workspace null, misaligned or smaller than %zu bytes", need);
-  const Split s = split_row(dtype, D);
-  const int threads = threads_of(s, kBwdThreads), blocks = T ? blocks_of(T * H, s, threads, kBwdBlocks) : 0;
+  const Split s = split_row(dtype, D, kBwdPieces);
+  const int threads = threads_of(s, kBwdThreads), blocks = T ? blocks_of(T * H, s, threads, kBwdPieces, kBwdBlocks) : 0;
   a.weight = weight; a.weight_bf16 = weight_dtype == MOE_BF16; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd); a.rows = T * H; a.heads = H; a.dim = D;
   a.lanes = s.lanes; a.waves = s.waves; a.per_token = divisor(H); a.per_dim = 1.0f / static_cast<float>(D);
   a.partial = wanted ? static_cast<float*>(ws) : nullptr; a.want_dw = dweight != nullptr; a.want_db = dbias != nullptr;
   hipStream_t st = static_cast<hipStream_t>(stream);
   begin_call("moe_norm_bwd", st);
-  if (blocks) launch_norm<true>(a, s, dtype, mean != nullptr, blocks, threads, st);
+  if (blocks) launch_bwd(a, s, dtype, mean != nullptr, blocks, threads, st);
   if (wanted)
     MOE_LAUNCH("norm_join", norm_join_kernel, dim3(ceil_div(D, kJoinColumns), dbias ? 2 : 1), dim3(kJoinThreads), 0, st, a.partial, blocks, D, dweight, dbias,
                weight_dtype == MOE_BF16);

@@ -21,6 +21,7 @@ template <> struct Piece<bf16_t, 8> {
 #pragma unroll
     for (int q = 0; q < 4; ++q) w[q] = pack_bf16x2(v[2 * q], v[2 * q + 1]);
   }
+  __device__ __forceinline__ void hide() { asm volatile("" : "+v"(w)); }   // what was computed from it before is not kept for what follows
   __device__ __forceinline__ Piece of_lane(int lane) const {
     Piece o;
 #pragma unroll
