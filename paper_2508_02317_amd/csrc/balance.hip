@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
         top = fmaxf(top, e[p][q]);
       }
     }
-    request(t + step);
+    if (base + step < a.T) request(t + step);
     top = lanes_max(top, a.lanes);
     const float from = top == -INFINITY ? 0.0f : top;  // a row without a finite logit has no probabilities
     float total = 0.0f;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
         sums[1] += share[p][q] * e[p][q];
       }
     }
-    request(t + step);
+    if (base + step < a.T) request(t + step);
     // the sum of exp(z - lse) is 1 but for the rounding of lse, which dividing by it takes out of the probabilities
     const float total = lanes_sum(sums[0], a.lanes), scale = total == 0.0f ? 0.0f : 1.0f / total, mean = lanes_sum(sums[1], a.lanes) * scale;
 #pragma unroll

@@ -18,7 +18,7 @@ namespace {
 constexpr int kMaxDim = 16384;
 constexpr int kFwdPieces = 4, kBwdPieces = 2;          // 16-byte pieces of a row that one lane holds; of shorter rows, several at once
 constexpr int kFwdThreads = 256, kBwdThreads = 512, kMaxThreads = 1024;   // at least; a row of more waves has a workgroup of them
-constexpr int kFwdBlocks = 2048, kBwdBlocks = 256;     // at most
+constexpr int kFwdBlocks = 4096, kBwdBlocks = 256;     // at most
 constexpr int kJoinColumns = 64, kJoinThreads = 1024;
 
 struct Rows {                                          // [T, H, D] with any strides of tokens and heads
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a) {
         }
       }
     }
-    request(base + all);
+    if (base + all < a.rows) request(base + all);
     sums(total, a.lanes, a.waves, me.wave, turn);
 #pragma unroll
     for (int u = 0; u < U; ++u) {

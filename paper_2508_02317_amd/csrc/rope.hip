@@ -53,33 +53,53 @@ template <int N> __device__ __forceinline__ void load_table(float (&v)[N], const
 }
 
 // ---- positions with several axes ---------------------------------------------------------------------------
-// Pair i turns by the position on its axis, positions[axis_i, t].  Which axis is two bits a pair, in the kernel's arguments; a lane looks its pairs'
-// up once.  Where all pairs of every lane share an axis (`whole`) the lane's part of the table is contiguous as ever, else its pairs are fetched one by one.
+// Pair i turns by the position on its axis, positions[axis_i, t].  Which axis is two bits a pair, in the kernel's arguments; a lane looks its pairs' up once.
+// WHOLE: the pairs of every lane share an axis, so its part of the table is contiguous as ever (three axes of 16, 24 and 24 pairs: 8192 tokens of 32 + 4 heads 28.9
+// us, 28.6 with one axis).  Else a lane reads its part of every axis' row and each pair takes its own: 40960 tokens 126.5 us, 130.7 where each pair was fetched
+// by itself, and 8192 tokens 31.7 and 35.3.
 struct OneAxis {};
-struct ManyAxes {
-  int n, whole;
+template <bool WHOLE> struct ManyAxes {
+  int n;
   uint32_t bits[kMaxRopePairs / 16];
 };
+template <class A> constexpr bool kManyAxes = !std::is_same_v<A, OneAxis>;
 // the axes of n consecutive pairs from `pair` on (a multiple of n, which divides 16)
-__device__ __forceinline__ uint32_t axes_of(const ManyAxes& x, int pair) { return x.bits[pair / 16] >> (2 * (pair % 16)); }
+template <bool WHOLE> __device__ __forceinline__ uint32_t axes_of(const ManyAxes<WHOLE>& x, int pair) { return x.bits[pair / 16] >> (2 * (pair % 16)); }
 
-// N/2 or N table values of a lane's pairs
-template <int M> __device__ __forceinline__ void load_axes(float (&c)[M], float (&s)[M], const RotateArgs& a, const ManyAxes& x, uint32_t axes, int pair, long t, int half) {
-  const ScalarInts positions = scalar_ints(a.positions);
-  int p[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) p[i] = min(max(positions[static_cast<long>(min(i, x.n - 1)) * a.T + t], 0), a.n_pos - 1);
-  auto row = [&](uint32_t axis) { const int lo = axis & 1 ? p[1] : p[0], hi = axis & 1 ? p[3] : p[2]; return static_cast<long>(axis & 2 ? hi : lo) * half + pair; };
-  if (x.whole) {
-    const long at = row(axes);
+// The table's values of M consecutive pairs
+template <int M, bool WHOLE>
+__device__ __forceinline__ void load_axes(float (&c)[M], float (&s)[M], const RotateArgs& a, const ManyAxes<WHOLE>& x, uint32_t axes, int pair, long t, int half) {
+  auto row = [&](int position) { return static_cast<long>(min(max(position, 0), a.n_pos - 1)) * half + pair; };
+  if constexpr (WHOLE) {
+    const long at = row(a.positions[static_cast<long>(axes & 3) * a.T + t]);
     load_table(c, a.cos + at);
     load_table(s, a.sin + at);
   } else {
+    const ScalarInts positions = scalar_ints(a.positions);
+    auto axis = [&](int i) { return row(positions[static_cast<long>(min(i, x.n - 1)) * a.T + t]); };
+    float cc[3][M], ss[3][M];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const long at = axis(i);
+      load_table(cc[i], a.cos + at);
+      load_table(ss[i], a.sin + at);
+    }
 #pragma unroll
     for (int q = 0; q < M; ++q) {
-      const long at = row(axes >> (2 * q)) + q;
-      c[q] = a.cos[at];
-      s[q] = a.sin[at];
+      const uint32_t k = axes >> (2 * q) & 3;
+      c[q] = k == 0 ? cc[0][q] : k == 1 ? cc[1][q] : cc[2][q];
+      s[q] = k == 0 ? ss[0][q] : k == 1 ? ss[1][q] : ss[2][q];
+    }
+    if (x.n > 3) {
+      const long at = axis(3);
+      load_table(cc[0], a.cos + at);
+      load_table(ss[0], a.sin + at);
+#pragma unroll
+      for (int q = 0; q < M; ++q) {
+        const bool last = (axes >> (2 * q) & 3) == 3;
+        c[q] = last ? cc[0][q] : c[q];
+        s[q] = last ? ss[0][q] : s[q];
+      }
     }
   }
 }
@@ -90,7 +110,7 @@ template <int M> __device__ __forceinline__ void load_axes(float (&c)[M], float 
 // row of each, moves 256-byte pieces: 40960 tokens of 32 + 4 heads 142 us, as it is 124.)
 template <class E, int N, int CACHE /* 0: none, 1: elements as they are, 2: 8-bit blocks */, class Axes>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, Axes axes, int lanes, int heads_per_block) {
-  constexpr bool kMany = std::is_same_v<Axes, ManyAxes>;
+  constexpr bool kMany = kManyAxes<Axes>;
   const int lane = static_cast<int>(threadIdx.x) & 63, chunk = lane & (lanes - 1), sub = lane / lanes, abreast = 64 / lanes;
   if (chunk * N >= a.D) return;                        // lanes of the power of two that a head row has no elements for
   const int half = a.rot / 2;
@@ -335,14 +355,15 @@ int32_t check_heads(const char* who, int dtype, int T, int D, int rot) {
 }
 
 // pair_axis [rot / 2] as the kernel takes it, for lanes of n elements
-int32_t take_axes(const char* who, int n_axes, const uint8_t* pair_axis, int rot, int interleaved, int n, ManyAxes* out) {
+int32_t take_axes(const char* who, int n_axes, const uint8_t* pair_axis, int rot, int interleaved, int n, ManyAxes<false>* out, bool* whole) {
   MOE_REQUIRE(rot == 0 || pair_axis, MOE_ERR_INVALID_ARG, "%s: a rotation needs the axis of every pair", who);
   const int per_lane = interleaved ? n / 2 : n;
-  *out = ManyAxes{n_axes, 1, {}};
+  *out = ManyAxes<false>{n_axes, {}};
+  *whole = true;
   for (int i = 0; i < rot / 2; ++i) {
     MOE_REQUIRE(pair_axis[i] < n_axes, MOE_ERR_INVALID_ARG, "%s: pair %d is on axis %d of %d", who, i, pair_axis[i], n_axes);
     out->bits[i / 16] |= static_cast<uint32_t>(pair_axis[i]) << (2 * (i % 16));
-    if (pair_axis[i] != pair_axis[i / per_lane * per_lane]) out->whole = 0;
+    if (pair_axis[i] != pair_axis[i / per_lane * per_lane]) *whole = false;
   }
   return MOE_OK;
 }
@@ -367,16 +388,19 @@ int32_t rope(const char* who, const char* name, int back, const void* q, int64_t
   a.interleaved = interleaved != 0; a.back = back; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.k_out = k_out; a.ko_stride_t = ko_stride_t; a.ko_stride_h = ko_stride_h; a.stream = static_cast<hipStream_t>(stream);
   const bool many = n_axes != 0;
-  ManyAxes axes{};
+  bool whole = true;
+  ManyAxes<false> axes{};
   if (many)
-    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_BF16 || D > 256 ? 8 : 4, &axes)) return rc;
+    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_BF16 || D > 256 ? 8 : 4, &axes, &whole)) return rc;
   auto launch = [&](auto x) {
     if (dtype == MOE_BF16) launch_rotate<bf16_t, 8, 0>(name, a, x);
     else if (D <= 256) launch_rotate<float, 4, 0>(name, a, x);
     else launch_rotate<float, 8, 0>(name, a, x);
   };
   begin_call(who, a.stream);
-  if (many) launch(axes); else launch(OneAxis{});
+  if (!many) launch(OneAxis{});
+  else if (whole) launch(__builtin_bit_cast(ManyAxes<true>, axes));
+  else launch(axes);
   return end_call();
 }
 
@@ -461,16 +485,19 @@ static int32_t cache_write(const char* who, const char* entry, const moe_kv_cach
   a.interleaved = interleaved != 0; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.slots = slots; a.cache = *cache; a.stream = static_cast<hipStream_t>(stream);
   const bool many = n_axes != 0;
-  ManyAxes axes{};
+  bool whole = true;
+  ManyAxes<false> axes{};
   if (many)
-    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_F32 ? 4 : 8, &axes)) return rc;
+    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_F32 ? 4 : 8, &axes, &whole)) return rc;
   auto launch = [&](auto x) {
     if (cache->dtype == MOE_F32) launch_rotate<float, 4, 1>(who, a, x);
     else if (cache->dtype == MOE_BF16) launch_rotate<bf16_t, 8, 1>(who, a, x);
     else launch_rotate<bf16_t, 8, 2>(who, a, x);
   };
   begin_call(entry, a.stream);
-  if (many) launch(axes); else launch(OneAxis{});
+  if (!many) launch(OneAxis{});
+  else if (whole) launch(__builtin_bit_cast(ManyAxes<true>, axes));
+  else launch(axes);
   return end_call();
 }
 
