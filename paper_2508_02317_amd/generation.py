@@ -5,7 +5,7 @@ transformer block over it.
     token    projection -> moe_kv_cache_write -> moe_paged_attn_decode -> projection
 
 The projections are plain library products; rotation, cache and the attention of single tokens are calls into libmoe on the current
-stream.  Which pages a sequence has is decided here, on the host, and reaches the device as four small tensors per step and layer, each
+stream; positions may have several axes.  Which pages a sequence has is decided here, on the host, and reaches the device as four small tensors per step and layer, each
 a copy that the host waits for.
 """
 import math
@@ -49,6 +49,23 @@ def rope_amplitude(factor):
     return 1.0 if factor <= 1.0 else 0.1 * math.log(factor) + 1.0
 
 
+def rope_axes(sections, cycled=False):
+    """The axis of every pair of a head's elements, for the calls that rotate by positions of several axes (time, height, width): sections[a] pairs of axis a,
+    the axes one after the other, or with `cycled` taking turns for as long as each has pairs left.  All pairs share one ladder of frequencies unless the
+    table is made from others: torch.cat([rope_frequencies(2 * n) for n in sections]) gives each section its own."""
+    if not 1 <= len(sections) <= 4 or min(sections) < 0:
+        raise ValueError("one to four sections of 0 or more pairs are possible, got %r" % (sections,))
+    if not cycled:
+        return bytes(a for a, n in enumerate(sections) for _ in range(n))
+    left, order = list(sections), []
+    while any(left):
+        for a in range(len(left)):
+            if left[a]:
+                left[a] -= 1
+                order.append(a)
+    return bytes(order)
+
+
 class PagedKVCache:
     """Keys and values of one attention layer in pages of page_size tokens, and the pages of every sequence.
 
@@ -67,15 +84,16 @@ class PagedKVCache:
         self.page_size, self.device = page_size, torch.device(device)
         self.free = list(range(pages - 1, -1, -1))
         self.pages_of, self.length = {}, {}
+        self.ahead = {}                                # by how much a sequence's next position is larger than its length (positions of several axes)
 
     def open(self, seq):
         if seq in self.length:
             raise ValueError("sequence %r is open" % (seq,))
-        self.pages_of[seq], self.length[seq] = [], 0
+        self.pages_of[seq], self.length[seq], self.ahead[seq] = [], 0, 0
 
     def close(self, seq):
         self.free.extend(reversed(self.pages_of.pop(seq)))
-        del self.length[seq]
+        del self.length[seq], self.ahead[seq]
 
     def grow(self, seqs, counts):
         """Places for counts[i] new tokens of seqs[i] -> slots [sum] i64, positions [sum] i32, pages [B, widest] i32, lens [B] i32, all on
@@ -118,15 +136,37 @@ class PagedKVCache:
 
 class CachedAttention:
     """The attention half of a block: y = W_out attention(rope(q), rope(k), v) with [q | k | v] = x W_qkv^T, the keys and values of earlier tokens in a
-    PagedKVCache.  w_qkv [(heads + 2 kv_heads) dim, d], w_out [d, heads dim]; cos, sin [n_pos, rot / 2] f32 (moe_rope_table)."""
+    PagedKVCache.  w_qkv [(heads + 2 kv_heads) dim, d], w_out [d, heads dim]; cos, sin [n_pos, rot / 2] f32 (moe_rope_table).
+    axes: the axis of every pair (rope_axes), for positions of several axes: a chunk of text has the next ones on all axes, pictures and video come with theirs."""
 
-    def __init__(self, cache, heads, w_qkv, w_out, cos, sin, interleaved=False, window=0):
+    def __init__(self, cache, heads, w_qkv, w_out, cos, sin, interleaved=False, window=0, axes=None):
         self.cache, self.heads, self.kv_heads, self.dim = cache, heads, cache.view.heads, cache.view.dim
         self.w_qkv, self.w_out, self.cos, self.sin, self.interleaved, self.window = w_qkv, w_out, cos, sin, interleaved, window
         if w_qkv.shape[0] != (heads + 2 * self.kv_heads) * self.dim or w_out.shape[1] != heads * self.dim:
             raise ValueError("w_qkv must have (heads + 2 kv_heads) dim rows and w_out heads dim columns")
+        if axes is not None and len(axes) != cos.shape[1]:
+            raise ValueError("axes must name the axis of each of the %d pairs" % cos.shape[1])
+        self.axes, self.n_axes = axes, 0 if axes is None else max(axes) + 1
 
-    def _step(self, x, seqs, counts, attend):
+    def _on_axes(self, seqs, counts, positions):
+        """Positions [axes, T] of the new tokens on the host, and how far every sequence's next position is ahead of its length after them: one larger than
+        the largest position of the chunk."""
+        first = [self.cache.length[s] + self.cache.ahead[s] for s in seqs]
+        if positions is None:
+            along = [p for at, n in zip(first, counts) for p in range(at, at + n)]
+            positions = torch.tensor(along, dtype=torch.int32).expand(self.n_axes, len(along))
+        elif positions.is_cuda or positions.dtype not in (torch.int32, torch.int64) or positions.shape != (self.n_axes, sum(counts)):
+            raise ValueError("positions must be whole numbers [%d, %d] on the host" % (self.n_axes, sum(counts)))
+        if positions.numel() and not 0 <= int(positions.min()) <= int(positions.max()) < self.cos.shape[0]:
+            raise ValueError("positions must lie in the rotation table, which ends at %d" % self.cos.shape[0])
+        ahead, at = [], 0
+        for s, n, before in zip(seqs, counts, first):
+            after = int(positions[:, at:at + n].max()) + 1 if n else before
+            ahead.append(after - self.cache.length[s] - n)
+            at += n
+        return positions.to(torch.int32).contiguous(), ahead
+
+    def _step(self, x, seqs, counts, attend, positions=None):
         """Projections around attend(q, pages, lens) -> [T, heads, dim] with the rows of x stored: q their rotated queries [T, heads, dim], a view of the
         projection's output, pages and lens those of the sequences.  What does not fit is refused before a sequence has grown, and where anything
         raises after that (memory that runs out, a call that refuses), the growth is taken back: no sequence keeps places that were not written."""
@@ -135,26 +175,37 @@ class CachedAttention:
             raise ValueError("rows of %d elements for %d new tokens are wanted, got %s" % (d, sum(counts), tuple(x.shape)))
         if x.dtype is not self.w_qkv.dtype or x.device != self.w_qkv.device:
             raise TypeError("rows must be %s on %s like the weights, got %s on %s" % (self.w_qkv.dtype, self.w_qkv.device, x.dtype, x.device))
-        if max((self.cache.length[s] + n for s, n in zip(seqs, counts)), default=0) > self.cos.shape[0]:
-            raise ValueError("the rotation table ends at position %d" % self.cos.shape[0])
+        if self.axes is None:
+            if positions is not None:
+                raise ValueError("positions are given where there are several axes")
+            if max((self.cache.length[s] + n for s, n in zip(seqs, counts)), default=0) > self.cos.shape[0]:
+                raise ValueError("the rotation table ends at position %d" % self.cos.shape[0])
+        else:
+            on_axes, ahead = self._on_axes(seqs, counts, positions)
         slots, positions, pages, lens = self.cache.grow(seqs, counts)
         try:
             qkv = torch.mm(x, self.w_qkv.t()).view(len(x), self.heads + 2 * self.kv_heads, self.dim)
             q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
-            q = L.moe_kv_cache_write(self.cache.view, k, v, slots, q, positions, self.cos, self.sin, self.interleaved, q_out=q)
-            return torch.mm(attend(q, pages, lens).view(len(x), self.heads * self.dim), self.w_out.t())
+            if self.axes is None:
+                q = L.moe_kv_cache_write(self.cache.view, k, v, slots, q, positions, self.cos, self.sin, self.interleaved, q_out=q)
+            else:
+                q = L.moe_kv_cache_write_axes(self.cache.view, k, v, slots, q, on_axes.to(x.device), self.cos, self.sin, self.axes, self.interleaved, q_out=q)
+            y = torch.mm(attend(q, pages, lens).view(len(x), self.heads * self.dim), self.w_out.t())
         except BaseException:
             self.cache.shrink(seqs, counts)
             raise
+        if self.axes is not None:
+            self.cache.ahead.update(zip(seqs, ahead))
+        return y
 
     def token(self, x, seqs):
         """One new token x[i] of every sequence seqs[i] -> [B, d]."""
         return self._step(x, seqs, [1] * len(seqs), lambda q, pages, lens: L.moe_paged_attn_decode(q, self.cache.view, pages, lens, window=self.window)[0])
 
-    def prompt(self, x, seqs, counts):
+    def prompt(self, x, seqs, counts, positions=None):
         """counts[i] new tokens of seqs[i], their rows of x one sequence after the other -> [sum(counts), d].  Every token attends to what its
-        sequence has in the cache up to itself."""
-        return self._step(x, seqs, counts, lambda q, pages, lens: self._attend_prompt(q, pages, counts, [self.cache.length[s] for s in seqs]))
+        sequence has in the cache up to itself.  positions [axes, sum(counts)] on the host, where there are several axes and the chunk is not text alone."""
+        return self._step(x, seqs, counts, lambda q, pages, lens: self._attend_prompt(q, pages, counts, [self.cache.length[s] for s in seqs]), positions)
 
     def _attend_prompt(self, q, pages, counts, ends):
         starts = torch.tensor([0] + ends, dtype=torch.int32).cumsum(0, dtype=torch.int32).to(q.device)

@@ -10,6 +10,9 @@ Backward: moe_grouped_gemm_swiglu_bwd_gather -> moe_unpermute_combine_fwd (unit 
 and, with weight_in_forward (the default of the gathered path), the combine weight is applied inside the forward
 products (act and yp leave scaled by it), so the forward combine is a plain sum and the backward finds w * act written.
 
+With balance or z given, moe_balance_loss_fwd follows the routing and moe_balance_loss_bwd adds its gradient to that of the logits.  NormedMoE puts the norm
+and the residual stream in front.
+
 Nothing is computed here; every step is a call into libmoe on the current stream, with no
 host synchronisation in between, and no allocation after construction.
 """
@@ -27,13 +30,18 @@ class MoELayer:
     """
 
     def __init__(self, T, d, E, k, f, dtype, w_gate, w_up, w_down, renorm=1, prerouted=False,
-                 save_gu=True, device="cuda", w_router=None, gather=False, weight_in_forward=None):
+                 save_gu=True, device="cuda", w_router=None, gather=False, weight_in_forward=None, balance=None, z=None):
         """w_router [E, d], if given, makes the layer start from hidden states: forward() computes the logits
-        itself and backward() also returns the router's weight gradient and adds the router term to dx."""
+        itself and backward() also returns the router's weight gradient and adds the router term to dx.
+        balance, z: weights of the router's balance loss and z loss in the loss whose gradient backward() gives (both None: no such losses); forward()
+        leaves the two, unweighted, in `losses` and counts and mean probabilities of the tokens that are valid in `valid_counts` and `importance`."""
         assert not prerouted or k == 1
         assert w_router is None or not prerouted
+        assert not prerouted or (balance is None and z is None)
         self.w_router = w_router
         self.gather = gather
+        self.has_losses = balance is not None or z is not None
+        self.balance, self.z, self.valid = balance or 0.0, z or 0.0, None
         self.weight_in_forward = gather if weight_in_forward is None else bool(weight_in_forward)
         assert gather or not self.weight_in_forward, "the weight can ride in the forward products only on the gathered path"
         self.T, self.d, self.E, self.k, self.f = T, d, E, k, f
@@ -70,10 +78,16 @@ class MoELayer:
             L.lib.moe_grouped_gemm_swiglu_bwd_workspace_bytes(code, P, d, f, E, int(save_gu)),
             L.lib.moe_grouped_gemm_swiglu_fwd_gather_workspace_bytes(code, P, d, f, E) if gather else 0,
             L.lib.moe_grouped_gemm_swiglu_bwd_gather_workspace_bytes(code, P, d, f, E, int(save_gu)) if gather else 0,
+            L.lib.moe_balance_loss_fwd_workspace_bytes(T, E, k) if self.has_losses else 0,
             256)
+        if self.has_losses:
+            self.losses, self.valid_counts, self.importance, self.lse = f32(2), i32(E + 1), f32(E), f32(T)
         self.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
 
-    def forward(self, x, logits=None, topk_idx=None, topk_w=None):
+    def forward(self, x, logits=None, topk_idx=None, topk_w=None, valid=None):
+        """valid [T] bool, if given: the tokens that count in the router's losses (padding is routed all the same)."""
+        if valid is not None and not self.has_losses:
+            raise ValueError("valid tokens are named where the router has losses")
         self.x = x
         if self.prerouted:
             self.topk_idx.copy_(topk_idx.view(self.T, 1))
@@ -84,6 +98,9 @@ class MoELayer:
                 logits = L.moe_router_logits(x, self.w_router, out=self.logits, ws=self.ws)
             L.moe_route_topk(logits, self.k, self.renorm,
                              out=(self.topk_idx, self.topk_w, self.counts, self.offsets), ws=self.ws)
+            if self.has_losses:
+                self.valid = valid
+                L.moe_balance_loss_fwd(logits, self.topk_idx, valid, out=(self.losses, self.valid_counts, self.importance, self.lse), ws=self.ws)
         if self.gather:
             L.moe_permute(None, self.topk_idx, self.offsets, self.E, out=(None, self.row_of_pair, self.pair_of_row), ws=self.ws)
             L.moe_grouped_gemm_swiglu_fwd_gather(x, self.k, self.pair_of_row, self.w_gate, self.w_up, self.w_down, self.offsets,
@@ -114,6 +131,36 @@ class MoELayer:
             if self.w_router is not None:
                 logits = self.logits
             L.moe_route_topk_bwd(self.dw, self.topk_w, self.topk_idx, logits, self.E, self.renorm, out=self.dlogits)
+            if self.has_losses:
+                L.moe_balance_loss_bwd(logits, self.valid_counts, self.lse, self.k, self.balance, self.z, valid=self.valid, add=self.dlogits, out=self.dlogits)
             if self.w_router is not None:
                 L.moe_router_bwd(self.dlogits, self.x, self.w_router, dx=self.dx, out_dw=self.dw_router, ws=self.ws)
         return self.dx, self.dw_gate, self.dw_up, self.dw_down, self.dlogits
+
+
+class NormedMoE:
+    """The feed-forward half of a block on a residual stream: h = x + stream, y = moe(norm(h)).  The caller's next half adds y to h.
+
+    moe: an MoELayer that starts from hidden states (w_router); weight, bias [d]: the norm's (None: 1 and 0)."""
+
+    def __init__(self, moe, weight=None, bias=None, eps=1e-6, rms=True):
+        assert moe.w_router is not None
+        self.moe, self.weight, self.bias, self.eps, self.rms = moe, weight, bias, eps, rms
+        dev, T, d = moe.ws.device, moe.T, moe.d
+        el, f32 = lambda: torch.empty((T, d), dtype=moe.dtype, device=dev), lambda: torch.empty(T, dtype=torch.float32, device=dev)
+        self.normed, self.h, self.dh = el(), el(), el()
+        self.mean, self.rstd = None if rms else f32(), f32()
+        like = lambda t: None if t is None else torch.empty_like(t)
+        self.dweight, self.dbias = like(weight), like(bias)
+        self.ws = torch.empty(max(L.lib.moe_norm_bwd_workspace_bytes(T, 1, d), 256), dtype=torch.uint8, device=dev)
+
+    def forward(self, x, stream, valid=None):
+        """-> y, h"""
+        L.moe_norm_fwd(x, self.weight, self.bias, self.eps, self.rms, stream, out=(self.normed, self.h, self.mean, self.rstd))
+        return self.moe.forward(self.normed, valid=valid), self.h
+
+    def backward(self, dy, dh=None):
+        """Gradients of y and, by the stream, of h -> the gradient of both x and stream; the weights' are in dweight, dbias and the MoE layer's."""
+        dx = self.moe.backward(dy)[0]
+        L.moe_norm_bwd(dx, self.h, self.rstd, self.mean, self.weight, dh, out=(self.dh, self.dweight, self.dbias), ws=self.ws)
+        return self.dh
