@@ -339,7 +339,7 @@ int32_t moe_rope_axes_bwd(const void* dq, int64_t q_stride_t, int64_t q_stride_h
  *   of 16 bytes; the other tensors alike, each with its own strides.  residual and sum come together or are both NULL.
  *   weight, bias [D] of type weight_dtype (MOE_F32, or MOE_BF16), or NULL: 1 and 0.
  *   mean, rstd [T, H] f32 out, or NULL; mean is not written when rms != 0.
- *   y may be x, and sum may be x or residual, with the same strides; other overlaps are not allowed.
+ *   y and sum may each be x or residual (not the same one), with the same strides; other overlaps are not allowed.
  * Backward of y with respect to h, for the upstream gradient dy:
  *   g = dy weight,  xh = (h - m) r,  dx = r (g - mean(g) - xh mean(g xh)) + add   (without mean(g) for the rms norm);
  *   dweight = sum over rows of dy xh,  dbias = sum over rows of dy, in fp32, rounded once to weight_dtype, overwritten.
@@ -374,7 +374,8 @@ int32_t moe_norm_bwd(const void* dy, int64_t dy_stride_t, int64_t dy_stride_h, c
  *   and add[t, e] alone for a token that is not valid.
  *   counts and lse as the forward call wrote them; dlosses [2] f32 (device), or NULL: ones; add [T, E] f32 (e.g. from moe_route_topk_bwd; may be
  *   dlogits), or NULL: zeros; dlogits [T, E] f32 out, every element written.
- * The order of all sums depends on the sizes only.  Limits as for moe_route_topk; all tensors but valid 16-byte aligned.
+ * The order of all sums depends on the sizes only.  Limits as for moe_route_topk.  Tensors need no more alignment than their elements have, so rows of any
+ * length may be taken from larger tensors.
  */
 size_t moe_balance_loss_fwd_workspace_bytes(int T, int E, int k);
 int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int E, int k, float* losses,

@@ -14,7 +14,7 @@ namespace moe {
 
 namespace {
 
-constexpr int kPieces = 2;                             // of 16 bytes that a lane has of a row, if the row has more than 64 lanes' worth: as many as it takes
+constexpr int kPieces = 2;                             // of 16 bytes that a lane has of a row, while 64 lanes suffice for it
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -364,19 +364,12 @@ __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
   }
 }
 
-// How the E columns of a row are dealt out: kPieces pieces a lane where the row has as many
-struct Split { int row, lanes, pieces; };
-Split split_columns(int E) {
-  const int all = ceil_div(E, 4);
-  Split s{4 * all, 1, 1};
-  while (s.lanes < 64 && s.lanes * kPieces < all) s.lanes *= 2;
-  while (s.lanes * s.pieces < all) s.pieces *= 2;
-  return s;
-}
 int fwd_blocks(int T, int E) {
-  const int rows = kFwdThreads / split_columns(E).lanes, n = T / rows + (T % rows != 0);
+  const int rows = kFwdThreads / split_columns(E, kPieces).lanes, n = T / rows + (T % rows != 0);
   return n < 1 ? 1 : n < kFwdBlocks ? n : kFwdBlocks;
 }
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 int32_t check_balance(const char* who, int T, int E, int k) {
   MOE_REQUIRE(T >= 0 && E > 0 && k > 0, MOE_ERR_INVALID_ARG, "%s: need T >= 0, E > 0, k > 0 (T=%d E=%d k=%d)", who, T, E, k);
@@ -404,18 +397,18 @@ extern "C" size_t moe_balance_loss_fwd_workspace_bytes(int T, int E, int k) {
   (void)k;
   if (T < 0 || E <= 0 || E > kMaxExperts) return 0;
   const size_t blocks = fwd_blocks(T, E);
-  return align_up(blocks * (2 * static_cast<size_t>(split_columns(E).row) + 2) * 4, 16) + kHeadBytes;
+  return align_up(blocks * (2 * static_cast<size_t>(split_columns(E, kPieces).row) + 2) * 4, 16) + kHeadBytes;
 }
 
 extern "C" int32_t moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int E, int k, float* losses, int32_t* counts,
                                         float* importance, float* lse, void* ws, size_t ws_bytes, void* stream) {
   if (int32_t rc = check_balance("balance_loss_fwd", T, E, k)) return rc;
   MOE_REQUIRE(losses && counts && importance && (T == 0 || (logits && topk_idx && lse)), MOE_ERR_INVALID_ARG, "balance_loss_fwd: null pointer");
-  MOE_REQUIRE(aligned16(logits) && aligned16(topk_idx) && aligned16(losses) && aligned16(counts) && aligned16(importance) && aligned16(lse), MOE_ERR_INVALID_ARG,
-              "balance_loss_fwd: tensors must be 16-byte aligned");
+  MOE_REQUIRE(aligned4(logits) && aligned4(topk_idx) && aligned4(losses) && aligned4(counts) && aligned4(importance) && aligned4(lse), MOE_ERR_INVALID_ARG,
+              "balance_loss_fwd: tensors must be 4-byte aligned");
   const size_t need = moe_balance_loss_fwd_workspace_bytes(T, E, k);
   MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "balance_loss_fwd: workspace null, misaligned or smaller than %zu bytes", need);
-  const Split s = split_columns(E);
+  const ColumnSplit s = split_columns(E, kPieces);
   const int blocks = fwd_blocks(T, E);
   FwdArgs a{logits, topk_idx, valid, losses, importance, lse, counts, T, E, k, s.lanes, s.row, divisor(k), nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   a.joined = static_cast<uint32_t*>(ws);
@@ -448,9 +441,9 @@ extern "C" int32_t moe_balance_loss_bwd(const float* logits, const int32_t* coun
   if (int32_t rc = check_balance("balance_loss_bwd", T, E, k)) return rc;
   if (T == 0) return MOE_OK;
   MOE_REQUIRE(logits && counts && lse && dlogits, MOE_ERR_INVALID_ARG, "balance_loss_bwd: null pointer");
-  MOE_REQUIRE(aligned16(logits) && aligned16(counts) && aligned16(lse) && aligned16(dlosses) && aligned16(add) && aligned16(dlogits), MOE_ERR_INVALID_ARG,
-              "balance_loss_bwd: tensors must be 16-byte aligned");
-  const Split s = split_columns(E);
+  MOE_REQUIRE(aligned4(logits) && aligned4(counts) && aligned4(lse) && aligned4(dlosses) && aligned4(add) && aligned4(dlogits), MOE_ERR_INVALID_ARG,
+              "balance_loss_bwd: tensors must be 4-byte aligned");
+  const ColumnSplit s = split_columns(E, kPieces);
   BwdArgs a{logits, counts, lse, valid, dlosses, add, dlogits, T, E, k, s.lanes, balance, z};
   const int rows = kBwdThreads / s.lanes, blocks = T / rows + (T % rows != 0);
   hipStream_t st = static_cast<hipStream_t>(stream);

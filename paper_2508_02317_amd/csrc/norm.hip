@@ -362,31 +362,15 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float* pa
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) sum += run[i][threadIdx.x];
-    if (bf16) static_cast<bf16_t*>(dst)[mine] = f32_to_bf16(sum);
+    if (bf16) static_cast<bf16_t*>(dst)[mine] = static_cast<bf16_t>(pack_bf16x2(sum, 0.0f));   // NaN stays NaN
     else static_cast<float*>(dst)[mine] = sum;
   }
 }
 
-// How rows of D elements are dealt out to lanes.
-struct Split { int lanes, waves, pieces; };
-Split split_row(int dtype, int D, int most) {
-  const int pieces = D / (16 / elem_size(dtype));
-  Split s{1, 1, 1};
-  while (s.lanes < 64 && s.lanes < pieces) s.lanes *= 2;
-  while (s.waves * 64 * most < pieces && s.waves * 64 < kMaxThreads) s.waves *= 2;
-  while (s.lanes * s.waves * s.pieces < pieces) s.pieces *= 2;
-  return s;
-}
-constexpr int rows_at_once(int pieces, int most) { return pieces < most ? most / pieces : 1; }
-int threads_of(const Split& s, int least) { return s.waves * 64 > least ? s.waves * 64 : least; }
-int groups_of(const Split& s, int threads) { return s.waves > 1 ? threads / 64 / s.waves : threads / s.lanes; }
-int blocks_of(int rows, const Split& s, int threads, int pieces, int most) {
-  const int step = groups_of(s, threads) * rows_at_once(s.pieces, pieces), n = rows / step + (rows % step != 0);
-  return n < most ? n : most;
-}
+RowSplit split_dim(int dtype, int D, int most) { return split_row(D / (16 / elem_size(dtype)), most); }
 
 // f(element type, elements of a piece, pieces of a lane) of a split
-template <class F> void with_split(const Split& s, int dtype, F f) {
+template <class F> void with_split(const RowSplit& s, int dtype, F f) {
   using std::integral_constant;
   auto typed = [&](auto e, auto n) {
     if (s.pieces == 1) f(e, n, integral_constant<int, 1>{});
@@ -396,7 +380,7 @@ template <class F> void with_split(const Split& s, int dtype, F f) {
   if (dtype == MOE_BF16) typed(bf16_t{}, integral_constant<int, 8>{});
   else typed(float{}, integral_constant<int, 4>{});
 }
-void launch_fwd(const NormArgs& a, const Split& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
+void launch_fwd(const NormArgs& a, const RowSplit& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
   with_split(s, dtype, [&](auto e, auto n, auto p) {
     auto launch = [&](auto kind, auto with_sum) {
       typedef decltype(e) E;
@@ -407,7 +391,7 @@ void launch_fwd(const NormArgs& a, const Split& s, int dtype, bool layer, int bl
     if (a.residual.p) kinds(std::true_type{}); else kinds(std::false_type{});
   });
 }
-void launch_bwd(const NormArgs& a, const Split& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
+void launch_bwd(const NormArgs& a, const RowSplit& s, int dtype, bool layer, int blocks, int threads, hipStream_t st) {
   const int units = threads / 64 / a.waves;
   const size_t lds = (a.want_dw || a.want_db) && units > 1 ? static_cast<size_t>(units / 2) * a.dim * 4 : 0;
   with_split(s, dtype, [&](auto e, auto n, auto p) {
@@ -464,7 +448,7 @@ extern "C" int32_t moe_norm_fwd(const void* x, int64_t x_stride_t, int64_t x_str
   a.x = rows(x, x_stride_t, x_stride_h); a.residual = rows(residual, r_stride_t, r_stride_h); a.sum = rows(sum, s_stride_t, s_stride_h); a.y = rows(y, y_stride_t, y_stride_h);
   MOE_REQUIRE(rows_ok(dtype, a.x) && rows_ok(dtype, a.y) && (!residual || (rows_ok(dtype, a.residual) && rows_ok(dtype, a.sum))) && aligned16(weight) && aligned16(bias),
               MOE_ERR_INVALID_ARG, "norm_fwd: tensors must be 16-byte aligned and strides multiples of 16 bytes");
-  const Split s = split_row(dtype, D, kFwdPieces);
+  const RowSplit s = split_dim(dtype, D, kFwdPieces);
   const int threads = threads_of(s, kFwdThreads);
   a.weight = weight; a.bias = bias; a.weight_bf16 = weight_dtype == MOE_BF16; a.mean = mean; a.rstd = rstd; a.rows = T * H; a.heads = H; a.dim = D;
   a.lanes = s.lanes; a.waves = s.waves; a.per_token = divisor(H); a.eps = eps; a.per_dim = 1.0f / static_cast<float>(D);
@@ -494,7 +478,7 @@ extern "C" int32_t moe_norm_bwd(const void* dy, int64_t dy_stride_t, int64_t dy_
               aligned16(dbias), MOE_ERR_INVALID_ARG, "norm_bwd: tensors must be 16-byte aligned and strides multiples of 16 bytes");
   const size_t need = moe_norm_bwd_workspace_bytes(T, H, D);
   MOE_REQUIRE(!wanted || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE, "norm_bwd: workspace null, misaligned or smaller than %zu bytes", need);
-  const Split s = split_row(dtype, D, kBwdPieces);
+  const RowSplit s = split_dim(dtype, D, kBwdPieces);
   const int threads = threads_of(s, kBwdThreads), blocks = T ? blocks_of(T * H, s, threads, kBwdPieces, kBwdBlocks) : 0;
   a.weight = weight; a.weight_bf16 = weight_dtype == MOE_BF16; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd); a.rows = T * H; a.heads = H; a.dim = D;
   a.lanes = s.lanes; a.waves = s.waves; a.per_token = divisor(H); a.per_dim = 1.0f / static_cast<float>(D);

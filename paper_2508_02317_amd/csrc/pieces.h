@@ -1,6 +1,7 @@
 // A lane's share of a row: 16 consecutive bytes (rope.hip, norm.hip, balance.hip), and what rows in lanes need.
 #pragma once
 #include "moe_common.h"
+#include "row_plan.h"
 
 namespace moe {
 
@@ -77,14 +78,5 @@ template <class F> __device__ __forceinline__ float lanes_fold(float v, int lane
 }
 __device__ __forceinline__ float lanes_sum(float v, int lanes) { return lanes_fold(v, lanes, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float lanes_max(float v, int lanes) { return lanes_fold(v, lanes, [](float a, float b) { return fmaxf(a, b); }); }
-
-// n / d for 0 <= n < 2^31 by a multiplication: mul = ceil(2^(32 + shift) / d) - 2^32 with 2^(shift - 1) < d <= 2^shift
-struct Divisor { uint32_t mul, shift; };
-inline Divisor divisor(uint32_t d) {
-  uint32_t shift = 0;
-  while ((uint64_t{1} << shift) < d) ++shift;
-  return {static_cast<uint32_t>((((uint64_t{1} << shift) - d) << 32) / d + 1), shift};
-}
-__device__ __forceinline__ uint32_t divide(uint32_t n, Divisor d) { return (__umulhi(n, d.mul) + n) >> d.shift; }
 
 }  // namespace moe

@@ -144,8 +144,9 @@ class CachedAttention:
         self.w_qkv, self.w_out, self.cos, self.sin, self.interleaved, self.window = w_qkv, w_out, cos, sin, interleaved, window
         if w_qkv.shape[0] != (heads + 2 * self.kv_heads) * self.dim or w_out.shape[1] != heads * self.dim:
             raise ValueError("w_qkv must have (heads + 2 kv_heads) dim rows and w_out heads dim columns")
-        if axes is not None and len(axes) != cos.shape[1]:
-            raise ValueError("axes must name the axis of each of the %d pairs" % cos.shape[1])
+        axes = None if axes is None else bytes(axes)
+        if axes is not None and (len(axes) != cos.shape[1] or not axes or max(axes) > 3):
+            raise ValueError("axes must name the axis, 0 to 3, of each of the %d pairs" % cos.shape[1])
         self.axes, self.n_axes = axes, 0 if axes is None else max(axes) + 1
 
     def _on_axes(self, seqs, counts, positions):

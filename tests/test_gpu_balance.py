@@ -170,6 +170,25 @@ def test_elements_beyond_32_bits():
     assert (np.abs(to_np(g[-3:]) - want) <= 200 * U * p * (share + 1) / T).all()
 
 
+def test_rows_taken_from_a_larger_tensor():
+    # rows of an odd length that start at any multiple of four bytes
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    for E in (13, 37, 130):
+        z, idx, _, add = (None if t is None else to_dev(t) for t in make(90, E, 3, E))
+        whole, more = torch.full((93, E), float("nan"), device="cuda"), torch.full((93, E), float("nan"), device="cuda")
+        for first in (1, 2, 3):
+            zz, aa = whole[first:first + 90], more[first:first + 90]
+            zz.copy_(z)
+            aa.copy_(add)
+            ref, got = L.moe_balance_loss_fwd(z, idx), L.moe_balance_loss_fwd(zz, idx)
+            assert all(torch.equal(p, q) for p, q in zip(ref, got))
+            g = L.moe_balance_loss_bwd(z, ref[1], ref[3], 3, 0.1, 0.2, add=add)
+            out = torch.full((93, E), 7.0, device="cuda")
+            assert torch.equal(L.moe_balance_loss_bwd(zz, got[1], got[3], 3, 0.1, 0.2, add=aa, out=out[first:first + 90]), g)
+            assert (out[:first] == 7).all() and (out[first + 90:] == 7).all()
+
+
 @pytest.mark.parametrize("compiled", [True, False])
 def test_both_ways_of_marshalling_and_what_they_refuse(monkeypatch, compiled):
     import torch

@@ -141,6 +141,9 @@ def test_views_of_larger_tensors_and_in_place(dtype):
             d, h, a = dy.clone(), dense[1].clone(), res.clone()
             got = L.moe_norm_bwd(d, h, dense[3], dense[2], w, add=a, out=((d, h, a)[alias], torch.empty_like(w), torch.empty_like(b)))
             assert same(grads, got), alias
+        p, s = whole[:, 1:H + 1].clone(), res.clone()
+        got = L.moe_norm_fwd(p, w, b, rms=rms, residual=s, out=(s, p, dense[2], dense[3]))      # y over the residual, the sum over x
+        assert torch.equal(s, dense[0]) and torch.equal(p, dense[1])
         s = res.clone()
         got = L.moe_norm_fwd(x, w, b, rms=rms, residual=s, out=(x, s, dense[2], dense[3]))      # y over x, the sum over the residual
         assert torch.equal(x, dense[0]) and torch.equal(s, dense[1]) and torch.equal(whole[:, 0], before[:, 0]) and torch.equal(whole[:, H + 1], before[:, H + 1])

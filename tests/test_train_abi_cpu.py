@@ -81,6 +81,7 @@ def test_norm_refuses_what_only_one_direction_has(L):
 
 
 def test_balance_refuses(L):
+    ODD = 18                                           # 4-byte alignment is all that is asked for
     fwd = lambda **kw: list(dict(dict(z=ONE, idx=ONE, valid=None, T=4, E=8, k=2, losses=ONE, counts=ONE, imp=ONE, lse=ONE, ws=ONE, ws_bytes=1 << 20, stream=None), **kw).values())
     bwd = lambda **kw: list(dict(dict(z=ONE, counts=ONE, lse=ONE, valid=None, T=4, E=8, k=2, a=1.0, b=1.0, dl=None, add=None, out=ONE, stream=None), **kw).values())
     for bad, status in ((dict(T=-1), "INVALID_ARG"), (dict(E=0), "INVALID_ARG"), (dict(k=0), "INVALID_ARG"), (dict(k=9), "INVALID_ARG"), (dict(E=1025), "UNSUPPORTED"),
