@@ -84,6 +84,11 @@ template <bool TAIL> __device__ __forceinline__ void store(const float (&v)[4], 
   }
 }
 
+// exp of a difference of logits that is near or below 0, by the hardware's power of two: the product's rounding is an error of 2^-24 |x|, as the
+// difference's own is, in probabilities that are the smaller the larger it is.  (With the library's expf, three times the instructions: 40960 tokens of 128 experts 25.3 us, 23.7
+// as it is; 8192 of 1024 35.8 and 33.6.  Outputs' errors against 64 bits 1.0e-7 with either.)
+__device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
 __device__ __forceinline__ double block_sum(double v, double* scratch) {   // scratch: one of each wave; the result in thread 0
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -160,10 +165,7 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
     for (int p = 0; p < P; ++p) {
       place<TAIL>(e[p], x[p], (p * a.lanes + lane) * 4, a.E, -INFINITY);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (!there) e[p][q] = -INFINITY;               // padding may hold anything
-        top = fmaxf(top, e[p][q]);
-      }
+      for (int q = 0; q < 4; ++q) top = fmaxf(top, e[p][q]);
     }
     if (base + step < a.T) request(t + step);
     top = lanes_max(top, a.lanes);
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
     for (int p = 0; p < P; ++p)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        e[p][q] = expf(e[p][q] - from);
+        e[p][q] = exp_near(e[p][q] - from);
         total += e[p][q];
       }
     total = lanes_sum(total, a.lanes);
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[p][q] += e[p][q] * scale;
+      for (int q = 0; q < 4; ++q) acc[p][q] += there ? e[p][q] * scale : 0.0f;   // padding may hold anything
     if (lane == 0 && t < a.T) {
       a.lse[t] = lse;
       n += there;
@@ -345,7 +347,7 @@ __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
       if constexpr (ADD) place<TAIL>(out[p], more[p], c, a.E, 0.0f);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        e[p][q] = any ? expf(e[p][q] - lse) : 0.0f;
+        e[p][q] = any ? exp_near(e[p][q] - lse) : 0.0f;
         if constexpr (!ADD) out[p][q] = 0.0f;
         sums[0] += e[p][q];
         sums[1] += share[p][q] * e[p][q];

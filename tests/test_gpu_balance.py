@@ -1,7 +1,8 @@
 """The router's losses on the GPU against the fp64 oracle, element by element; counts exactly.
 
-Tolerances, derived, with u = 2^-24.  A probability exp(z - top) / total: the difference is off by u |z - top|, exp by 2 u, the total by its terms' errors and a sum
-of depth at most 16 + 6, the reciprocal and the product by 2 u: (2 R + 32) u relative, R the largest |z - top| of the row's finite logits.
+Tolerances, derived, with u = 2^-24.  A probability exp(z - top) / total: the difference and its product with log2 e are off by u |z - top| each, the power of two by
+2 u, the total by its terms' errors (the large ones have a small |z - top|) and a sum of depth at most 16 + 6, the reciprocal and the product by 2 u:
+(2 R + 32) u relative, R the largest |z - top| of the row's finite logits.
   lse = top + log(total): that of the total, 3 u of log, u of the sum: (R + 28 + 3 |log total| + |lse|) u.
   importance: all terms are positive: (2 R + 32) u and the depth of the sum: T / 256 + 4 in a lane, 6 + 8 in a workgroup, 64 + 16 in the join.
   losses[0]: the same and 4 u.  losses[1]: 2 |lse| times lse's error, and the depth's.
