@@ -93,14 +93,19 @@ template <bool TAIL> __device__ __forceinline__ void store(const float (&v)[4], 
 // as it is; 8192 of 1024 35.8 and 33.6.  Outputs' errors against 64 bits 1.0e-7 with either.)
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-__device__ __forceinline__ double block_sum(double v, double* scratch) {   // scratch: one of each wave; the result in thread 0
+// Over the first WAVES waves of a workgroup; scratch: one of each of them, the result in thread 0
+template <int WAVES> __device__ __forceinline__ double block_sum(double v, double* scratch) {
+  if (static_cast<int>(threadIdx.x) < 64 * WAVES) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+  }
   __syncthreads();
   double all = 0.0;
-  if (threadIdx.x == 0)
-    for (int i = 0; i < static_cast<int>(blockDim.x) >> 6; ++i) all += scratch[i];
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) all += scratch[i];
+  }
   return all;
 }
 
@@ -230,7 +235,7 @@ __global__ __launch_bounds__(kFwdThreads) void balance_fwd_kernel(FwdArgs a) {
     }
   }
   if (ONE) {
-    balance = block_sum(balance, scratch);
+    balance = block_sum<kFwdWaves>(balance, scratch);
     if (threadIdx.x == 0) finish(a, balance, z_sum, n);
   } else if (threadIdx.x == 0) {
     a.z_of[blockIdx.x] = z_sum;
@@ -246,7 +251,8 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, i
   constexpr int kWaves = kJoinThreads / 64;
   __shared__ float sums[kWaves][kJoinLanes * 4];
   __shared__ int32_t counts[kWaves][kJoinLanes * 4], n_all;
-  __shared__ double scratch[kWaves], z_all;
+  constexpr int kSumWaves = kJoinLanes * 4 / 64;       // a thread for each of the workgroup's columns
+  __shared__ double scratch[kSumWaves], z_all;
   const int l = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6, lane = l & (lanes - 1), runs = kJoinThreads / lanes;
   const int e = (blockIdx.x * lanes + lane) * 4;
   f32x4 sum = {};
@@ -293,7 +299,7 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(FwdArgs a, i
     for (int w = 0; w < kWaves; ++w) { s += sums[w][threadIdx.x]; c += counts[w][threadIdx.x]; }
     balance = finish_expert(a, mine, s, c, n);
   }
-  balance = block_sum(balance, scratch);
+  balance = block_sum<kSumWaves>(balance, scratch);
   if (threadIdx.x != 0) return;
   if (gridDim.x > 1) {
     __hip_atomic_store(&a.loss_of[blockIdx.x], balance, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

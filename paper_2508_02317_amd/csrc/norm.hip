@@ -27,7 +27,7 @@ constexpr int kFwdThreads = 256, kBwdThreads = 512, kMaxThreads = 1024;   // at 
 // at most: forward 40960 rows with residual 116.9 us with 2048, 112.2 with 4096, 111.1 with 8192, without residual 58.1, 56.4 and 61.4; back 256 leave the fewest
 // sums (8192 rows 28.2, 31.8 with 512; 40960 rows 109.6 and 112.0)
 constexpr int kFwdBlocks = 4096, kBwdBlocks = 256;
-constexpr int kJoinColumns = 64, kJoinThreads = 1024;
+constexpr int kJoinColumns = 32, kJoinThreads = 512;    // 64 and 1024: 8192 rows back 28.0 us, 27.8 as it is
 
 struct Rows {                                          // [T, H, D] with any strides of tokens and heads
   void* p;
