@@ -125,7 +125,8 @@ class PagedKVCache:
 
     def shrink(self, seqs, counts):
         """Takes the last counts[i] tokens of seqs[i] back, and the pages that held nothing else: after a grow of the same arguments everything, the
-        order of the free pages included, is as it was before.  Nothing changes where the arguments do not fit (ValueError)."""
+        order of the free pages included, is as it was before.  Nothing changes where the arguments do not fit (ValueError).  Where positions have
+        several axes, a sequence's next position falls by as many."""
         if len(set(seqs)) != len(seqs) or len(counts) != len(seqs) or not all(0 <= n <= self.length[s] for s, n in zip(seqs, counts)):
             raise ValueError("every sequence needs a number of tokens that it has")
         for s, n in zip(reversed(seqs), reversed(counts)):
@@ -156,13 +157,13 @@ class CachedAttention:
         if positions is None:
             along = [p for at, n in zip(first, counts) for p in range(at, at + n)]
             positions = torch.tensor(along, dtype=torch.int32).expand(self.n_axes, len(along))
-        elif positions.is_cuda or positions.dtype not in (torch.int32, torch.int64) or positions.shape != (self.n_axes, sum(counts)):
+        elif not isinstance(positions, torch.Tensor) or positions.is_cuda or positions.dtype not in (torch.int32, torch.int64) or positions.shape != (self.n_axes, sum(counts)):
             raise ValueError("positions must be whole numbers [%d, %d] on the host" % (self.n_axes, sum(counts)))
         if positions.numel() and not 0 <= int(positions.min()) <= int(positions.max()) < self.cos.shape[0]:
             raise ValueError("positions must lie in the rotation table, which ends at %d" % self.cos.shape[0])
         ahead, at = [], 0
         for s, n, before in zip(seqs, counts, first):
-            after = int(positions[:, at:at + n].max()) + 1 if n else before
+            after = int(positions[:, at:at + n].max()) + 1 if n > 0 else before     # (counts that do not fit are refused where the pages are handed out)
             ahead.append(after - self.cache.length[s] - n)
             at += n
         return positions.to(torch.int32).contiguous(), ahead

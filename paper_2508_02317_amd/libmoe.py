@@ -719,6 +719,18 @@ def moe_paged_attn_decode(q, cache, pages, lens, scale=None, window=0, out=None,
 # ---- positions with several axes, the norm, the router's losses ------------------------------------------------------
 # These refuse tensors that are not on the current device, whose stream the call goes to.
 
+if _raw_stream is not None:
+    _device_now = getattr(torch._C, "_cuda_getDevice", _current_device)   # torch.cuda.current_device() looks first whether torch has a device at all, 0.2 us
+
+    def _where():
+        """The current stream of the current device, and the device."""
+        device = _device_now()
+        return _raw_stream(device), device
+else:
+    def _where():
+        return _stream(), _current_device()
+
+
 def _on(t, name):
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
@@ -754,7 +766,7 @@ def _rope_axes(back, q, k, positions, cos, sin, pair_axis, interleaved, out):
     if out is None:
         out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
     if _marshal is not None:
-        _check(_marshal.rope_axes(back, q, k, positions, cos, sin, pair_axis, interleaved, out[0], out[1], _stream(), _current_device()))
+        _check(_marshal.rope_axes(back, q, k, positions, cos, sin, pair_axis, interleaved, out[0], out[1], *_where()))
         return out
     some = q if q is not None else k
     if some is None:
@@ -791,7 +803,7 @@ def moe_kv_cache_write_axes(cache, k, v, slots, q, positions, cos, sin, pair_axi
     if q is not None and q_out is None:
         q_out = torch.empty(q.shape, dtype=cache.dtype, device=q.device)
     if _marshal is not None:
-        _check(_marshal.kv_cache_write_axes(ref, cache.k.get_device(), k, v, slots, q, positions, cos, sin, pair_axis, interleaved, q_out, _stream(), _current_device()))
+        _check(_marshal.kv_cache_write_axes(ref, cache.k.get_device(), k, v, slots, q, positions, cos, sin, pair_axis, interleaved, q_out, *_where()))
         return q_out
     _on(cache.k, "cache")
     T, dt = k.shape[0], cache.dtype
@@ -851,7 +863,7 @@ def moe_norm_fwd(x, weight=None, bias=None, eps=1e-6, rms=False, residual=None, 
         out = mk(), None if residual is None else mk(), stat(not rms), stat(True)
     y, h, mean, rstd = out
     if _marshal is not None:
-        _check(_marshal.norm_fwd(x, weight, bias, eps, rms, residual, y, h, mean, rstd, _stream(), _current_device()))
+        _check(_marshal.norm_fwd(x, weight, bias, eps, rms, residual, y, h, mean, rstd, *_where()))
         return out
     if x is None or y is None:
         raise ValueError("x and y must be given")
@@ -875,7 +887,7 @@ def moe_norm_bwd(dy, x, rstd, mean=None, weight=None, add=None, with_weight=True
     if ws is None and (dweight is not None or dbias is not None):
         ws, _ = _ws(lib.moe_norm_bwd_workspace_bytes, (T, H, D), None, x.device)
     if _marshal is not None:
-        _check(_marshal.norm_bwd(dy, x, rstd, mean, weight, add, dx, dweight, dbias, ws, _stream(), _current_device()))
+        _check(_marshal.norm_bwd(dy, x, rstd, mean, weight, add, dx, dweight, dbias, ws, *_where()))
         return out
     if dy is None or dx is None or rstd is None:
         raise ValueError("dy, rstd and dx must be given")
@@ -912,7 +924,7 @@ def moe_balance_loss_fwd(logits, topk_idx, valid=None, out=None, ws=None):
     if ws is None:
         ws, _ = _ws(lib.moe_balance_loss_fwd_workspace_bytes, (T, E, k), None, logits.device)
     if _marshal is not None:
-        _check(_marshal.balance_loss_fwd(logits, topk_idx, valid, losses, counts, importance, lse, ws, _stream(), _current_device()))
+        _check(_marshal.balance_loss_fwd(logits, topk_idx, valid, losses, counts, importance, lse, ws, *_where()))
         return out
     p_logits, p_idx = _logits(logits), _flat(topk_idx, torch.int32, None, "topk_idx")
     if topk_idx.dim() != 2 or topk_idx.shape[0] != T:
@@ -931,7 +943,7 @@ def moe_balance_loss_bwd(logits, counts, lse, k, balance=1.0, z=0.0, dlosses=Non
     if out is None:
         out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
     if _marshal is not None:
-        _check(_marshal.balance_loss_bwd(logits, counts, lse, k, balance, z, dlosses, valid, add, out, _stream(), _current_device()))
+        _check(_marshal.balance_loss_bwd(logits, counts, lse, k, balance, z, dlosses, valid, add, out, *_where()))
         return out
     p_logits = _logits(logits)
     T, E = logits.shape

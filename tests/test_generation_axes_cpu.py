@@ -59,7 +59,11 @@ def test_positions_that_do_not_fit_change_nothing(on_axes, monkeypatch):
     a.prompt(torch.zeros(3, 32), ["a"], [3], torch.tensor([[0, 0, 0], [0, 0, 5], [0, 1, 0]]))
     before = state(cache), dict(cache.ahead)
     three = lambda v: torch.tensor(v).expand(3, -1)
-    for bad in (three([6, 40]), three([-1, 0]), three([6]), torch.zeros(2, 2, dtype=torch.int32), three([6.0, 7.0])):
+    for seqs, counts in ((['a', 'a'], [1, 1]), (['a'], [-1]), (['a'], []), (['a'], [1, 1])):
+        with pytest.raises(ValueError):
+            a.prompt(torch.zeros(sum(counts) if sum(counts) > 0 else 0, 32), seqs, counts)
+        assert before == (state(cache), cache.ahead)
+    for bad in ([[6, 7]] * 3, three([6, 40]), three([-1, 0]), three([6]), torch.zeros(2, 2, dtype=torch.int32), three([6.0, 7.0])):
         with pytest.raises(ValueError):
             a.prompt(torch.zeros(2, 32), ["a"], [2], bad)
         assert before == (state(cache), cache.ahead)

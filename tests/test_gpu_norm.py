@@ -149,6 +149,19 @@ def test_views_of_larger_tensors_and_in_place(dtype):
         assert torch.equal(x, dense[0]) and torch.equal(s, dense[1]) and torch.equal(whole[:, 0], before[:, 0]) and torch.equal(whole[:, H + 1], before[:, H + 1])
 
 
+def test_gradients_that_are_one_row_for_all():
+    # what the gradient of a sum is: a tensor without strides, beside an added one that is one row per token
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    x, res, dy, w, b = make(50, 4, 128, "bf16", 11)
+    out = L.moe_norm_fwd(x, w, b)
+    one, token = dy[:1, :1].expand(50, 4, 128), res[:, :1].expand(50, 4, 128)
+    ref = L.moe_norm_bwd(one.contiguous(), x, out[3], out[2], w, add=token.contiguous(), with_bias=True)
+    got = L.moe_norm_bwd(one, x, out[3], out[2], w, add=token, with_bias=True)
+    assert all(torch.equal(p, q) for p, q in zip(ref, got))
+    assert torch.equal(L.moe_norm_fwd(x, w, b, residual=token)[0], L.moe_norm_fwd(x, w, b, residual=token.contiguous())[0])
+
+
 def test_more_rows_than_workgroups_take_at_once():
     # long walks: sums over many rows, and rows of one lane
     from paper_2508_02317_amd import libmoe as L

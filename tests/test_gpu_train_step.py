@@ -236,6 +236,22 @@ def test_prompts_with_pictures_and_steps_after_them(eight_bit, sections, cycled)
     assert cache.length["a"] + cache.ahead["a"] == nxt["a"] + 3
 
 
+def test_steps_of_no_sequences_and_sequences_of_no_tokens_on_axes():
+    import torch
+    from paper_2508_02317_amd import generation as G
+    from paper_2508_02317_amd import libmoe as L
+    cos, sin = L.moe_rope_table(G.rope_frequencies(64).cuda(), 32)
+    cache = G.PagedKVCache(4, 16, 1, 64)
+    att = G.CachedAttention(cache, 1, torch.randn((192, 32), device="cuda").bfloat16(), torch.randn((32, 64), device="cuda").bfloat16(), cos, sin, axes=G.rope_axes((8, 12, 12)))
+    none = torch.zeros((0, 32), dtype=torch.bfloat16, device="cuda")
+    assert att.token(none, []).shape == (0, 32) and att.prompt(none, [], []).shape == (0, 32)
+    cache.open("a"); cache.open("b")
+    assert att.prompt(none, ["a"], [0], torch.zeros((3, 0), dtype=torch.int32)).shape == (0, 32) and cache.ahead == {"a": 0, "b": 0}
+    x = torch.randn((3, 32), device="cuda").bfloat16()
+    y = att.prompt(x, ["a", "b"], [0, 3])
+    assert y.shape == (3, 32) and y.isfinite().all() and cache.length == {"a": 0, "b": 3}
+
+
 def test_the_example_runs_with_pictures():
     import subprocess
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))

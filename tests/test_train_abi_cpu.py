@@ -107,6 +107,7 @@ def test_host_tensors_are_refused_by_name(L, monkeypatch, compiled):
         monkeypatch.setattr(L, "_marshal", None)
     monkeypatch.setattr(L, "_current_device", lambda: 0)
     monkeypatch.setattr(L, "_stream", lambda: 0)
+    monkeypatch.setattr(L, "_where", lambda: (0, 0))
     x, v = torch.zeros(4, 64), torch.zeros(4)
     with pytest.raises(ValueError, match="x must be a device tensor"):
         L.moe_norm_fwd(x)
