@@ -54,26 +54,47 @@ template <int N> __device__ __forceinline__ void load_table(float (&v)[N], const
 
 // ---- positions with several axes ---------------------------------------------------------------------------
 // Pair i turns by the position on its axis, positions[axis_i, t].  Which axis is two bits a pair, in the kernel's arguments; a lane looks its pairs' up once.
-// WHOLE: the pairs of every lane share an axis, so its part of the table is contiguous as ever (three axes of 16, 24 and 24 pairs: 8192 tokens of 32 + 4 heads 28.9
-// us, 28.6 with one axis).  Else a lane reads its part of every axis' row and each pair takes its own: 40960 tokens 126.5 us, 130.7 where each pair was fetched
-// by itself, and 8192 tokens 31.7 and 35.3.
+// MOST: the axes that the pairs of one lane have between them.  1: its part of the table is contiguous as ever (three axes of 16, 24 and 24 pairs: 8192 tokens of 32 + 4
+// heads 28.9 us, 28.6 with one axis).  2 (two axes, or sections that end inside a lane): it reads its part of two rows and each
+// pair takes its own, 30.9 us (31.7 reading that of all axes).  4 (any): that of all axes; in turn over three 31.8, 35.3 where each pair was fetched by itself, and 40960
+// tokens 127.1 and 130.7.
 struct OneAxis {};
-template <bool WHOLE> struct ManyAxes {
+template <int MOST> struct ManyAxes {
   int n;
   uint32_t bits[kMaxRopePairs / 16];
 };
 template <class A> constexpr bool kManyAxes = !std::is_same_v<A, OneAxis>;
 // the axes of n consecutive pairs from `pair` on (a multiple of n, which divides 16)
-template <bool WHOLE> __device__ __forceinline__ uint32_t axes_of(const ManyAxes<WHOLE>& x, int pair) { return x.bits[pair / 16] >> (2 * (pair % 16)); }
+template <int MOST> __device__ __forceinline__ uint32_t axes_of(const ManyAxes<MOST>& x, int pair) { return x.bits[pair / 16] >> (2 * (pair % 16)); }
 
 // The table's values of M consecutive pairs
-template <int M, bool WHOLE>
-__device__ __forceinline__ void load_axes(float (&c)[M], float (&s)[M], const RotateArgs& a, const ManyAxes<WHOLE>& x, uint32_t axes, int pair, long t, int half) {
+template <int M, int MOST>
+__device__ __forceinline__ void load_axes(float (&c)[M], float (&s)[M], const RotateArgs& a, const ManyAxes<MOST>& x, uint32_t axes, int pair, long t, int half) {
   auto row = [&](int position) { return static_cast<long>(min(max(position, 0), a.n_pos - 1)) * half + pair; };
-  if constexpr (WHOLE) {
+  if constexpr (MOST == 1) {
     const long at = row(a.positions[static_cast<long>(axes & 3) * a.T + t]);
     load_table(c, a.cos + at);
     load_table(s, a.sin + at);
+  } else if constexpr (MOST == 2) {
+    const uint32_t one = axes & 3;
+    uint32_t other = one;
+#pragma unroll
+    for (int q = 1; q < M; ++q) {
+      const uint32_t k = axes >> (2 * q) & 3;
+      other = k != one ? k : other;
+    }
+    const long first = row(a.positions[static_cast<long>(one) * a.T + t]), second = row(a.positions[static_cast<long>(other) * a.T + t]);
+    float cc[M], ss[M];
+    load_table(c, a.cos + first);
+    load_table(s, a.sin + first);
+    load_table(cc, a.cos + second);
+    load_table(ss, a.sin + second);
+#pragma unroll
+    for (int q = 1; q < M; ++q) {
+      const bool mine = (axes >> (2 * q) & 3) == one;
+      c[q] = mine ? c[q] : cc[q];
+      s[q] = mine ? s[q] : ss[q];
+    }
   } else {
     const ScalarInts positions = scalar_ints(a.positions);
     auto axis = [&](int i) { return row(positions[static_cast<long>(min(i, x.n - 1)) * a.T + t]); };
@@ -354,18 +375,28 @@ int32_t check_heads(const char* who, int dtype, int T, int D, int rot) {
   return MOE_OK;
 }
 
-// pair_axis [rot / 2] as the kernel takes it, for lanes of n elements
-int32_t take_axes(const char* who, int n_axes, const uint8_t* pair_axis, int rot, int interleaved, int n, ManyAxes<false>* out, bool* whole) {
+// pair_axis [rot / 2] as the kernel takes it, and how many axes the pairs of a lane of n elements have between them at most
+int32_t take_axes(const char* who, int n_axes, const uint8_t* pair_axis, int rot, int interleaved, int n, ManyAxes<4>* out, int* most) {
   MOE_REQUIRE(rot == 0 || pair_axis, MOE_ERR_INVALID_ARG, "%s: a rotation needs the axis of every pair", who);
   const int per_lane = interleaved ? n / 2 : n;
-  *out = ManyAxes<false>{n_axes, {}};
-  *whole = true;
+  *out = ManyAxes<4>{n_axes, {}};
+  *most = 1;
+  unsigned seen = 0;
   for (int i = 0; i < rot / 2; ++i) {
     MOE_REQUIRE(pair_axis[i] < n_axes, MOE_ERR_INVALID_ARG, "%s: pair %d is on axis %d of %d", who, i, pair_axis[i], n_axes);
     out->bits[i / 16] |= static_cast<uint32_t>(pair_axis[i]) << (2 * (i % 16));
-    if (pair_axis[i] != pair_axis[i / per_lane * per_lane]) *whole = false;
+    seen = (i % per_lane ? seen : 0u) | 1u << pair_axis[i];
+    const int axes = __builtin_popcount(seen);
+    *most = axes > *most ? axes : *most;
   }
   return MOE_OK;
+}
+// launch(the kind of axes that the kernels are made for)
+template <class F> void with_axes(int n_axes, int most, const ManyAxes<4>& axes, F launch) {
+  if (n_axes == 0) launch(OneAxis{});
+  else if (most == 1) launch(__builtin_bit_cast(ManyAxes<1>, axes));
+  else if (most == 2) launch(__builtin_bit_cast(ManyAxes<2>, axes));
+  else launch(axes);
 }
 
 int32_t rope(const char* who, const char* name, int back, const void* q, int64_t q_stride_t, int64_t q_stride_h, const void* k, int64_t k_stride_t,
@@ -387,20 +418,17 @@ int32_t rope(const char* who, const char* name, int back, const void* q, int64_t
   a.T = T; a.Hq = Hq; a.Hk = Hk; a.Hv = 0; a.D = D; a.rot = rot; a.positions = positions; a.cos = cos; a.sin = sin; a.n_pos = n_pos;
   a.interleaved = interleaved != 0; a.back = back; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.k_out = k_out; a.ko_stride_t = ko_stride_t; a.ko_stride_h = ko_stride_h; a.stream = static_cast<hipStream_t>(stream);
-  const bool many = n_axes != 0;
-  bool whole = true;
-  ManyAxes<false> axes{};
-  if (many)
-    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_BF16 || D > 256 ? 8 : 4, &axes, &whole)) return rc;
+  int most = 0;
+  ManyAxes<4> axes{};
+  if (n_axes != 0)
+    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_BF16 || D > 256 ? 8 : 4, &axes, &most)) return rc;
   auto launch = [&](auto x) {
     if (dtype == MOE_BF16) launch_rotate<bf16_t, 8, 0>(name, a, x);
     else if (D <= 256) launch_rotate<float, 4, 0>(name, a, x);
     else launch_rotate<float, 8, 0>(name, a, x);
   };
   begin_call(who, a.stream);
-  if (!many) launch(OneAxis{});
-  else if (whole) launch(__builtin_bit_cast(ManyAxes<true>, axes));
-  else launch(axes);
+  with_axes(n_axes, most, axes, launch);
   return end_call();
 }
 
@@ -484,20 +512,17 @@ static int32_t cache_write(const char* who, const char* entry, const moe_kv_cach
   a.T = T; a.Hq = Hq; a.Hk = a.Hv = cache->heads; a.D = cache->dim; a.rot = rot; a.positions = positions; a.cos = cos; a.sin = sin; a.n_pos = n_pos;
   a.interleaved = interleaved != 0; a.q_out = q_out; a.qo_stride_t = qo_stride_t; a.qo_stride_h = qo_stride_h;
   a.slots = slots; a.cache = *cache; a.stream = static_cast<hipStream_t>(stream);
-  const bool many = n_axes != 0;
-  bool whole = true;
-  ManyAxes<false> axes{};
-  if (many)
-    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_F32 ? 4 : 8, &axes, &whole)) return rc;
+  int most = 0;
+  ManyAxes<4> axes{};
+  if (n_axes != 0)
+    if (int32_t rc = take_axes(who, n_axes, pair_axis, rot, interleaved, dtype == MOE_F32 ? 4 : 8, &axes, &most)) return rc;
   auto launch = [&](auto x) {
     if (cache->dtype == MOE_F32) launch_rotate<float, 4, 1>(who, a, x);
     else if (cache->dtype == MOE_BF16) launch_rotate<bf16_t, 8, 1>(who, a, x);
     else launch_rotate<bf16_t, 8, 2>(who, a, x);
   };
   begin_call(entry, a.stream);
-  if (!many) launch(OneAxis{});
-  else if (whole) launch(__builtin_bit_cast(ManyAxes<true>, axes));
-  else launch(axes);
+  with_axes(n_axes, most, axes, launch);
   return end_call();
 }
 
