@@ -84,16 +84,18 @@ class PagedKVCache:
         self.page_size, self.device = page_size, torch.device(device)
         self.free = list(range(pages - 1, -1, -1))
         self.pages_of, self.length = {}, {}
-        self.ahead = {}                                # by how much a sequence's next position is larger than its length (positions of several axes)
+        # positions of several axes: by how much a sequence's next position is larger than its length; its chunks that came with positions, as
+        # (length and ahead before the chunk, the position that follows each of its tokens)
+        self.ahead, self.placed = {}, {}
 
     def open(self, seq):
         if seq in self.length:
             raise ValueError("sequence %r is open" % (seq,))
-        self.pages_of[seq], self.length[seq], self.ahead[seq] = [], 0, 0
+        self.pages_of[seq], self.length[seq], self.ahead[seq], self.placed[seq] = [], 0, 0, []
 
     def close(self, seq):
         self.free.extend(reversed(self.pages_of.pop(seq)))
-        del self.length[seq], self.ahead[seq]
+        del self.length[seq], self.ahead[seq], self.placed[seq]
 
     def grow(self, seqs, counts):
         """Places for counts[i] new tokens of seqs[i] -> slots [sum] i64, positions [sum] i32, pages [B, widest] i32, lens [B] i32, all on
@@ -125,14 +127,28 @@ class PagedKVCache:
 
     def shrink(self, seqs, counts):
         """Takes the last counts[i] tokens of seqs[i] back, and the pages that held nothing else: after a grow of the same arguments everything, the
-        order of the free pages included, is as it was before.  Nothing changes where the arguments do not fit (ValueError).  Where positions have
-        several axes, a sequence's next position falls by as many."""
+        order of the free pages included, is as it was before.  Nothing changes where the arguments do not fit (ValueError).  The next
+        position is again the one that followed the tokens that stay."""
         if len(set(seqs)) != len(seqs) or len(counts) != len(seqs) or not all(0 <= n <= self.length[s] for s, n in zip(seqs, counts)):
             raise ValueError("every sequence needs a number of tokens that it has")
         for s, n in zip(reversed(seqs), reversed(counts)):
             self.length[s] -= n
             while len(self.pages_of[s]) > -(-self.length[s] // self.page_size):
                 self.free.append(self.pages_of[s].pop())
+            placed = self.placed[s]
+            while placed and self.length[s] < placed[-1][0] + len(placed[-1][2]):
+                start, ahead, follows = placed.pop()
+                follows = follows[:max(self.length[s] - start, 0)]
+                if follows:
+                    placed.append((start, ahead, follows))
+                    ahead = follows[-1] - self.length[s]
+                self.ahead[s] = ahead
+
+    def place(self, seq, follows):
+        """The last len(follows) tokens of seq came with positions: follows[i] is the one that follows the first i + 1 of them."""
+        if follows:
+            self.placed[seq].append((self.length[seq] - len(follows), self.ahead[seq], follows))
+            self.ahead[seq] = follows[-1] - self.length[seq]
 
 
 class CachedAttention:
@@ -151,22 +167,21 @@ class CachedAttention:
         self.axes, self.n_axes = axes, 0 if axes is None else max(axes) + 1
 
     def _on_axes(self, seqs, counts, positions):
-        """Positions [axes, T] of the new tokens on the host, and how far every sequence's next position is ahead of its length after them: one larger than
-        the largest position of the chunk."""
-        first = [self.cache.length[s] + self.cache.ahead[s] for s in seqs]
+        """Positions [axes, T] of the new tokens on the host and, where they were given, the position that follows each token of every sequence: one larger
+        than the largest of its chunk so far."""
         if positions is None:
+            first = [self.cache.length[s] + self.cache.ahead[s] for s in seqs]
             along = [p for at, n in zip(first, counts) for p in range(at, at + n)]
-            positions = torch.tensor(along, dtype=torch.int32).expand(self.n_axes, len(along))
+            positions, follows = torch.tensor(along, dtype=torch.int32).expand(self.n_axes, len(along)), None
         elif not isinstance(positions, torch.Tensor) or positions.is_cuda or positions.dtype not in (torch.int32, torch.int64) or positions.shape != (self.n_axes, sum(counts)):
             raise ValueError("positions must be whole numbers [%d, %d] on the host" % (self.n_axes, sum(counts)))
+        else:                                          # (counts that do not fit are refused where the pages are handed out)
+            follows = []
+            if min(counts, default=0) >= 0:
+                follows = [(c.amax(0).cummax(0).values + 1).tolist() if c.numel() else [] for c in positions.long().split(list(counts), dim=1)]
         if positions.numel() and not 0 <= int(positions.min()) <= int(positions.max()) < self.cos.shape[0]:
             raise ValueError("positions must lie in the rotation table, which ends at %d" % self.cos.shape[0])
-        ahead, at = [], 0
-        for s, n, before in zip(seqs, counts, first):
-            after = int(positions[:, at:at + n].max()) + 1 if n > 0 else before     # (counts that do not fit are refused where the pages are handed out)
-            ahead.append(after - self.cache.length[s] - n)
-            at += n
-        return positions.to(torch.int32).contiguous(), ahead
+        return positions.to(torch.int32).contiguous(), follows
 
     def _step(self, x, seqs, counts, attend, positions=None):
         """Projections around attend(q, pages, lens) -> [T, heads, dim] with the rows of x stored: q their rotated queries [T, heads, dim], a view of the
@@ -183,7 +198,7 @@ class CachedAttention:
             if max((self.cache.length[s] + n for s, n in zip(seqs, counts)), default=0) > self.cos.shape[0]:
                 raise ValueError("the rotation table ends at position %d" % self.cos.shape[0])
         else:
-            on_axes, ahead = self._on_axes(seqs, counts, positions)
+            on_axes, follows = self._on_axes(seqs, counts, positions)
         slots, positions, pages, lens = self.cache.grow(seqs, counts)
         try:
             qkv = torch.mm(x, self.w_qkv.t()).view(len(x), self.heads + 2 * self.kv_heads, self.dim)
@@ -196,8 +211,9 @@ class CachedAttention:
         except BaseException:
             self.cache.shrink(seqs, counts)
             raise
-        if self.axes is not None:
-            self.cache.ahead.update(zip(seqs, ahead))
+        if self.axes is not None and follows is not None:
+            for s, after in zip(seqs, follows):
+                self.cache.place(s, after)
         return y
 
     def token(self, x, seqs):

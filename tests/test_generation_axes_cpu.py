@@ -79,3 +79,32 @@ def test_positions_that_do_not_fit_change_nothing(on_axes, monkeypatch):
         plain.prompt(torch.zeros(1, 32), ["a"], [1], torch.zeros(3, 1, dtype=torch.int32))
     with pytest.raises(ValueError):
         G.CachedAttention(cache, 2, torch.zeros(6 * 64, 32), torch.zeros(32, 2 * 64), torch.zeros(40, 32), torch.zeros(40, 32), axes=bytes(31))
+
+
+def test_tokens_taken_back_give_their_positions_back(on_axes):
+    """What shrink leaves goes on as if the tokens taken back had never been there: in the text behind a picture, in the picture and before it."""
+    a, cache = on_axes, on_axes.cache
+    cache.open("a"); cache.open("b")
+    rows = lambda n: torch.zeros(n, 32)
+    picture = torch.tensor([[4, 4, 4, 4], [4, 4, 5, 5], [4, 5, 4, 6]])
+    step = [lambda: a.prompt(rows(4), ["a"], [4]), lambda: a.prompt(rows(4), ["a"], [4], picture), lambda: a.token(rows(1), ["a"]),
+            lambda: a.prompt(rows(2), ["a"], [2], torch.tensor([[20, 3]] * 3)), lambda: a.token(rows(1), ["a"])]
+    for f in step:
+        f()
+    follows = [0, 1, 2, 3, 4, 5, 6, 6, 7, 8, 21, 21, 22]                            # position behind the first n tokens
+    a.seen.clear()
+    for length in (12, 11, 10, 9, 8, 7, 6, 5, 4, 2, 0):
+        cache.shrink(["a"], [cache.length["a"] - length])
+        a.prompt(rows(3), ["b", "a"], [1, 2])                                       # text goes on, and is taken back
+        assert a.seen.pop()[0][1:] == [follows[length], follows[length] + 1]
+        cache.shrink(["a", "b"], [2, 1])
+        assert cache.length == {"a": length, "b": 0} and cache.ahead == {"a": follows[length] - length, "b": 0}
+    assert cache.placed == {"a": [], "b": []}
+    for f in step:
+        f()
+    cache.shrink(["a"], [9])                                                        # over the second picture and all but none of the first
+    assert cache.ahead["a"] == 0 and cache.placed["a"] == []
+    with pytest.raises(ValueError):
+        cache.shrink(["a"], [5])
+    cache.close("a")
+    assert cache.placed == {"b": []} and cache.ahead == {"b": 0}
