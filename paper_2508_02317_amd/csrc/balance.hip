@@ -7,8 +7,8 @@
 // Bound by HBM and by launches: the logits are read once by each pass, the gradient (and what it is added to) once more.  A row belongs to `lanes` lanes of a
 // wave, so that several short rows lie side by side, and a lane has the same columns of all its rows: the sums over tokens stay in its registers.  They go over the
 // waves through LDS, as rows of the workspace to a second launch, and every step adds in a fixed order; counts are whole numbers, so their order is free.
-// Measured: 40960 tokens of 128 experts 23.4 us, three dependent launches: 8.5 (23 MB read; four fifths of the time are five dependent turns of a workgroup), 5.5 (one
-// workgroup adds 256 rows, 260 KB) and 9.4 (63 MB, 6.7 TB/s, part of it from the memory-side cache); 8192 tokens 15 to 16 (4.7, 5.4, 4.7); 8192 of 1024 experts 33.7;
+// Measured: 40960 tokens of 128 experts 23.1 us, three dependent launches: 8.6 (23 MB read; four fifths of the time are five dependent turns of a workgroup), 6.0 (one
+// workgroup adds 256 rows, 260 KB) and 9.7 (63 MB, 6.5 TB/s, part of it from the memory-side cache); 8192 tokens 14.7 to 16 (4.8, 6.0, 4.8); 8192 of 1024 experts 33.7;
 // 256 tokens of 8 experts, which one workgroup does alone, are bound by the host's two calls (8 to 9.5; 5.0 and 2.7 on the GPU).
 #include "moe_common.h"
 #include "pieces.h"
@@ -21,7 +21,7 @@ constexpr int kPieces = 2;                             // of 16 bytes that a lan
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 
-// 512 workgroups forward: 40960 tokens +1.2 us, 8192 of 1024 experts +3 (twice the rows to add)
+// 512 workgroups forward: 40960 tokens +1.2 us, 8192 of 1024 experts +3 (twice the rows to add); 128: 8192 tokens -0.5, 40960 +3.6, 8192 of 512 experts +1.7
 constexpr int kFwdThreads = 512, kFwdWaves = kFwdThreads / 64, kFwdBlocks = 256;
 constexpr int kBwdThreads = 512, kBwdBlocks = 512;     // 1024 workgroups: 40960 tokens +1.5 us, 8192 of 1024 experts +4
 constexpr size_t kHeadBytes = 512;                     // of the workspace: the join's counter and losses
