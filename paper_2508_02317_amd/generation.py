@@ -168,9 +168,9 @@ class CachedAttention:
 
     def _on_axes(self, seqs, counts, positions):
         """Positions [axes, T] of the new tokens on the host and, where they were given, the position that follows each token of every sequence: one larger
-        than the largest of its chunk so far."""
+        than the largest of the sequence so far, so that a picture may come in several chunks and its patches in any order."""
+        first = [self.cache.length[s] + self.cache.ahead[s] for s in seqs]
         if positions is None:
-            first = [self.cache.length[s] + self.cache.ahead[s] for s in seqs]
             along = [p for at, n in zip(first, counts) for p in range(at, at + n)]
             positions, follows = torch.tensor(along, dtype=torch.int32).expand(self.n_axes, len(along)), None
         elif not isinstance(positions, torch.Tensor) or positions.is_cuda or positions.dtype not in (torch.int32, torch.int64) or positions.shape != (self.n_axes, sum(counts)):
@@ -178,7 +178,8 @@ class CachedAttention:
         else:                                          # (counts that do not fit are refused where the pages are handed out)
             follows = []
             if min(counts, default=0) >= 0:
-                follows = [(c.amax(0).cummax(0).values + 1).tolist() if c.numel() else [] for c in positions.long().split(list(counts), dim=1)]
+                chunks = positions.long().split(list(counts), dim=1)
+                follows = [(c.amax(0).cummax(0).values + 1).clamp(min=at).tolist() if c.numel() else [] for at, c in zip(first, chunks)]
         if positions.numel() and not 0 <= int(positions.min()) <= int(positions.max()) < self.cos.shape[0]:
             raise ValueError("positions must lie in the rotation table, which ends at %d" % self.cos.shape[0])
         return positions.to(torch.int32).contiguous(), follows

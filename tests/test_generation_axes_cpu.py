@@ -108,3 +108,29 @@ def test_tokens_taken_back_give_their_positions_back(on_axes):
         cache.shrink(["a"], [5])
     cache.close("a")
     assert cache.placed == {"b": []} and cache.ahead == {"b": 0}
+
+
+@pytest.mark.parametrize("patches", [
+    [(0, i // 8, i % 8) for i in range(24)],                                        # in raster order
+    [(0, i // 8, i % 8) for i in range(19)],                                        # the same, ending inside a row
+    [(0, i % 3, i // 3) for i in range(24)],                                        # column by column
+    [(i // 4, 0, 9 - i % 4) for i in range(12)],                                    # frames, each from its last column on
+    [(0, 0, i) for i in (11, 3, 7, 0, 2)]])
+def test_what_follows_a_picture_is_the_same_however_it_is_cut(on_axes, patches):
+    """Behind the first n tokens of a sequence text goes on one behind the largest position that they have, in whichever chunks they came."""
+    a, cache = on_axes, on_axes.cache
+    rows = lambda n: torch.zeros(n, 32)
+    picture, n = torch.tensor(patches).t().contiguous() + 2, len(patches)
+    follows = [0, 1, 2] + (picture.amax(0).cummax(0).values + 1).tolist()           # behind two tokens of text and 0, 1, ... patches
+    for cut in range(n + 1):
+        for length in range(n + 2, -1, -1):
+            cache.open("a")
+            a.prompt(rows(2), ["a"], [2])
+            for part in (picture[:, :cut], picture[:, cut:]):
+                a.prompt(rows(part.shape[1]), ["a"], [part.shape[1]], part)
+            assert cache.length["a"] + cache.ahead["a"] == follows[-1], cut
+            cache.shrink(["a"], [n + 2 - length])
+            a.seen.clear()
+            a.token(rows(1), ["a"])
+            assert a.seen == [[[follows[length]]] * 3], (cut, length)
+            cache.close("a")
