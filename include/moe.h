@@ -371,7 +371,7 @@ int32_t moe_norm_bwd(const void* dy, int64_t dy_stride_t, int64_t dy_stride_h, c
  *   A logit of -inf has no probability; a row of nothing else counts as a token, with no probabilities, lse = -inf and no part in losses[1].
  * Backward of balance dlosses[0] losses[0] + z dlosses[1] losses[1], the counts being constants:
  *   dlogits[t, e] = add[t, e] + p[t, e] (balance dlosses[0] / n (s_e - sum_e' s_e' p[t, e']) + z dlosses[1] 2 / n lse[t]),  s_e = E counts[e] / (k n),
- *   and add[t, e] alone for a token that is not valid.
+ *   and add[t, e] alone, whatever dlosses holds, for a token that is not valid or has no probabilities.
  *   counts and lse as the forward call wrote them; dlosses [2] f32 (device), or NULL: ones; add [T, E] f32 (e.g. from moe_route_topk_bwd; may be
  *   dlogits), or NULL: zeros; dlogits [T, E] f32 out, every element written.
  * The order of all sums depends on the sizes only.  Limits as for moe_route_topk.  Tensors need no more alignment than their elements have, so rows of any

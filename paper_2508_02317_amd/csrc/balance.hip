@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
   for (long base = static_cast<long>(blockIdx.x) * groups; base < a.T; base += step, t += step) {
     const float lse = lse_next;
     const bool any = on != 0 && lse != -INFINITY;      // else the token does not count, or has no finite logit
-    const float level = any ? lse * to_z : 0.0f;
+    const float push = any ? to_balance : 0.0f, level = any ? lse * to_z : 0.0f;   // dlosses may be infinite or NaN
     float e[P][4], out[P][4], sums[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(kBwdThreads) void balance_bwd_kernel(BwdArgs a) {
     for (int p = 0; p < P; ++p) {
       const int c = (p * a.lanes + lane) * 4;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) out[p][q] += e[p][q] * scale * ((share[p][q] - mean) * to_balance + level);
+      for (int q = 0; q < 4; ++q) out[p][q] += e[p][q] * scale * ((share[p][q] - mean) * push + level);
       if (t < a.T && c < a.E) store<TAIL>(out[p], a.dlogits + t * a.E, c, a.E);
     }
   }

@@ -216,3 +216,20 @@ def test_both_ways_of_marshalling_and_what_they_refuse(monkeypatch, compiled):
         L.moe_balance_loss_bwd(z, counts, lse, 13)
     with pytest.raises(L.MoEError, match="workspace"):
         L.moe_balance_loss_fwd(z, idx, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def test_tokens_that_do_not_count_have_the_added_gradient_alone_whatever_the_losses_gradients_are():
+    # as where a scaled loss overflows: infinities and NaN arrive in dlosses
+    import torch
+    from paper_2508_02317_amd import libmoe as L
+    for T, E in ((40, 8), (700, 13), (300, 512)):
+        z, idx, valid, add = make(T, E, 2, E, padding=0.4)
+        z[3], valid[3] = -np.inf, True                                   # counts, and has no probabilities
+        plain = ~valid
+        plain[3] = True
+        out = L.moe_balance_loss_fwd(to_dev(z), to_dev(idx), to_dev(valid))
+        for dl in ((np.inf, 1.0), (1.0, -np.inf), (np.nan, np.nan)):
+            for more in (add, None):
+                g = to_np(L.moe_balance_loss_bwd(to_dev(z), out[1], out[3], 2, 0.1, 0.1, dlosses=to_dev(np.float32(dl)), valid=to_dev(valid), add=None if more is None else to_dev(more)))
+                assert np.array_equal(g[plain], np.zeros((plain.sum(), E)) if more is None else more[plain]), (T, E, dl)
+                assert not np.isfinite(g[~plain]).any(), (T, E, dl)
