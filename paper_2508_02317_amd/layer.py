@@ -34,14 +34,15 @@ class MoELayer:
         """w_router [E, d], if given, makes the layer start from hidden states: forward() computes the logits
         itself and backward() also returns the router's weight gradient and adds the router term to dx.
         balance, z: weights of the router's balance loss and z loss in the loss whose gradient backward() gives (both None: no such losses); forward()
-        leaves the two, unweighted, in `losses` and counts and mean probabilities of the tokens that are valid in `valid_counts` and `importance`."""
+        leaves the two, unweighted, in `losses` and counts and mean probabilities of the tokens that are valid in `valid_counts` and `importance`.
+        With such losses backward() takes the logits that forward() was given, which stay unchanged until then, unless it is given them again."""
         assert not prerouted or k == 1
         assert w_router is None or not prerouted
         assert not prerouted or (balance is None and z is None)
         self.w_router = w_router
         self.gather = gather
         self.has_losses = balance is not None or z is not None
-        self.balance, self.z, self.valid = balance or 0.0, z or 0.0, None
+        self.balance, self.z, self.valid, self.given_logits = balance or 0.0, z or 0.0, None, None
         self.weight_in_forward = gather if weight_in_forward is None else bool(weight_in_forward)
         assert gather or not self.weight_in_forward, "the weight can ride in the forward products only on the gathered path"
         self.T, self.d, self.E, self.k, self.f = T, d, E, k, f
@@ -99,7 +100,7 @@ class MoELayer:
             L.moe_route_topk(logits, self.k, self.renorm,
                              out=(self.topk_idx, self.topk_w, self.counts, self.offsets), ws=self.ws)
             if self.has_losses:
-                self.valid = valid
+                self.valid, self.given_logits = valid, logits
                 L.moe_balance_loss_fwd(logits, self.topk_idx, valid, out=(self.losses, self.valid_counts, self.importance, self.lse), ws=self.ws)
         if self.gather:
             L.moe_permute(None, self.topk_idx, self.offsets, self.E, out=(None, self.row_of_pair, self.pair_of_row), ws=self.ws)
@@ -116,6 +117,8 @@ class MoELayer:
         return self.y
 
     def backward(self, dy, logits=None):
+        if logits is None and self.has_losses:
+            logits = self.given_logits
         if self.gather:
             L.moe_grouped_gemm_swiglu_bwd_gather(dy, self.x, self.topk_w, self.pair_of_row, self.g, self.u, self.w_gate,
                                                  self.w_up, self.w_down, self.offsets,

@@ -258,3 +258,26 @@ def test_the_example_runs_with_pictures():
     r = subprocess.run([sys.executable, os.path.join(root, "examples", "generate.py"), "--seqs", "3", "--prompt", "80", "--tokens", "3", "--pictures"], capture_output=True, text=True,
                        timeout=100)
     assert r.returncode == 0 and "3 sequences" in r.stdout and "nan" not in r.stdout, r.stdout + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("renorm", [1, 0])
+@pytest.mark.parametrize("gather", [True, False])
+def test_losses_of_a_layer_that_is_given_its_logits(renorm, gather):
+    """backward() needs no logits: they are those that forward() had."""
+    import torch
+    from paper_2508_02317_amd.layer import MoELayer
+    T, d, E, k, f = 61, 64, 12, 3, 32
+    r = np.random.default_rng(2)
+    mk = lambda *s, scale=1.0: to_dev((scale * r.standard_normal(s)).astype(np.float32))
+    wg, wu, wd, x, dy, logits = mk(E, f, d, scale=0.1), mk(E, f, d, scale=0.1), mk(E, d, f, scale=0.1), mk(T, d), mk(T, d, scale=1.0 / T), mk(T, E)
+    valid = torch.arange(T, device="cuda") % 5 < 4
+    bare = MoELayer(T, d, E, k, f, torch.float32, wg, wu, wd, renorm=renorm, gather=gather)
+    y = bare.forward(x, logits=logits).clone()
+    ref = [t.clone() for t in bare.backward(dy, logits=logits)]
+    layer = MoELayer(T, d, E, k, f, torch.float32, wg, wu, wd, renorm=renorm, gather=gather, balance=0.3, z=0.05)
+    for given in (None, logits.clone()):
+        assert torch.equal(layer.forward(x, logits=logits, valid=valid), y)
+        got = layer.backward(dy) if given is None else layer.backward(dy, logits=given)
+        assert all(torch.equal(a, b) for a, b in zip(got[:4], ref[:4]))
+        more = O.balance_bwd(to_np(logits), to_np(layer.topk_idx), 0.3, 0.05, to_np(valid), add=to_np(ref[4]))
+        assert_close(to_np(got[4]), more, "f32", "dlogits")
