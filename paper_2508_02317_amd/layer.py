@@ -86,7 +86,7 @@ class MoELayer:
         self.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
 
     def forward(self, x, logits=None, topk_idx=None, topk_w=None, valid=None):
-        """valid [T] bool, if given: the tokens that count in the router's losses (padding is routed all the same)."""
+        """valid [T] bool, if given: the tokens that count in the router's losses (padding is routed all the same); backward() reads x and valid again."""
         if valid is not None and not self.has_losses:
             raise ValueError("valid tokens are named where the router has losses")
         self.x = x
@@ -142,7 +142,8 @@ class MoELayer:
 
 
 class NormedMoE:
-    """The feed-forward half of a block on a residual stream: h = x + stream, y = moe(norm(h)).  The caller's next half adds y to h.
+    """The feed-forward half of a block on a residual stream: h = x + stream, y = moe(norm(h)).  The caller's next half adds y to h, into a
+    tensor of its own: h is this object's and, like valid, has to stay as it is until backward() has read it.
 
     moe: an MoELayer that starts from hidden states (w_router); weight, bias [d]: the norm's (None: 1 and 0)."""
 

@@ -281,3 +281,24 @@ def test_losses_of_a_layer_that_is_given_its_logits(renorm, gather):
         assert all(torch.equal(a, b) for a, b in zip(got[:4], ref[:4]))
         more = O.balance_bwd(to_np(logits), to_np(layer.topk_idx), 0.3, 0.05, to_np(valid), add=to_np(ref[4]))
         assert_close(to_np(got[4]), more, "f32", "dlogits")
+
+
+def test_halves_on_one_residual_stream_keep_what_their_backward_passes_read():
+    """Two halves in a row: the second adds the first one's y to its stream in a buffer of its own, so the first's gradients are those that it has alone."""
+    import torch
+    T = 70
+    (t, make), (_, other) = half_block(T, 256, 16, 4, 128, "bf16", True, balance=0.1), half_block(T, 256, 16, 4, 128, "bf16", True, seed=5)
+    first, second = make(True), other(False)
+    y, h = first.forward(t["x"], t["stream"])
+    held = h.clone()
+    y2, h2 = second.forward(y, h)
+    assert torch.equal(h, held) and torch.equal(h2, (y.float() + h.float()).bfloat16())
+    g = second.backward(t["dy"], t["dh"]).clone()
+    dx = first.backward(g, g).clone()
+    t3, make3 = half_block(T, 256, 16, 4, 128, "bf16", True, balance=0.1)
+    third = make3(True)
+    third.forward(t3["x"], t3["stream"])
+    assert torch.equal(third.backward(g, g), dx)
+    for name in ("dweight", "dbias"):
+        assert torch.equal(getattr(third, name), getattr(first, name))
+    assert torch.equal(third.moe.dw_down, first.moe.dw_down) and torch.equal(third.moe.dw_router, first.moe.dw_router)
