@@ -7,9 +7,10 @@
 // Bound by HBM and by launches: the logits are read once by each pass, the gradient (and what it is added to) once more.  A row belongs to `lanes` lanes of a
 // wave, so that several short rows lie side by side, and a lane has the same columns of all its rows: the sums over tokens stay in its registers.  They go over the
 // waves through LDS, as rows of the workspace to a second launch, and every step adds in a fixed order; counts are whole numbers, so their order is free.
-// Measured: 40960 tokens of 128 experts 23.1 us, three dependent launches: 8.6 (23 MB read; four fifths of the time are five dependent turns of a workgroup), 6.0 (one
-// workgroup adds 256 rows, 260 KB) and 9.7 (63 MB, 6.5 TB/s, part of it from the memory-side cache); 8192 tokens 14.7 to 16 (4.8, 6.0, 4.8); 8192 of 1024 experts 33.7;
-// 256 tokens of 8 experts, which one workgroup does alone, are bound by the host's two calls (8 to 9.5; 5.0 and 2.7 on the GPU).
+// Measured, passes among others and in brackets the launches as the profiler sees each (together they come to more than a pass): 40960 tokens of 128 experts 23.1 to 23.3 us (9.0: 23 MB
+// read, four fifths of the time are five dependent turns of a workgroup with the loads of one turn in flight; 5.8: one workgroup adds 256 rows, 260 KB; 9.8: 63 MB, 6.5 TB/s, part of it
+// from the memory-side cache); 8192 tokens 14.7 to 16 (4.8, 6.0, 4.8); 8192 of 1024 experts 33.7; 256 tokens of 8 experts, which one workgroup does alone, are bound by the host's two
+// calls, 8 to 9.5 (4.8 and 2.5).
 #include "moe_common.h"
 #include "pieces.h"
 
@@ -17,7 +18,7 @@ namespace moe {
 
 namespace {
 
-constexpr int kPieces = 2;                             // of 16 bytes that a lane has of a row, while 64 lanes suffice for it: 40960 tokens of 128 experts 25.4 us, 26.7 with four, 28.8 with one
+constexpr int kPieces = 2;                             // of 16 bytes that a lane has of a row, while 64 lanes suffice for it: 40960 tokens of 128 experts +1.3 us with four, +3.4 with one
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -89,8 +90,8 @@ template <bool TAIL> __device__ __forceinline__ void store(const float (&v)[4], 
 }
 
 // exp of a difference of logits that is near or below 0, by the hardware's power of two: the product's rounding is an error of 2^-24 |x|, as the
-// difference's own is, in probabilities that are the smaller the larger it is.  (With the library's expf, three times the instructions: 40960 tokens of 128 experts 25.3 us, 23.7
-// as it is; 8192 of 1024 35.8 and 33.6.  Outputs' errors against 64 bits 1.0e-7 with either.)
+// difference's own is, in probabilities that are the smaller the larger it is.  (With the library's expf, three times the instructions: 40960 tokens of 128 experts +1.6 us,
+// 8192 of 1024 +2.2.  Outputs' errors against 64 bits 1.0e-7 with either.)
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // Over the first WAVES waves of a workgroup; scratch: one of each of them, the result in thread 0

@@ -10,7 +10,7 @@
 // h is rounded to the element type before the norm is taken of it: it is what the next layer adds to and what the backward pass reads.  Sums, statistics and
 // the gradients' sums are fp32; y, dx, dw and db are rounded once.
 // Measured in bf16 (a streaming copy moves 5.9 to 6.3 TB/s): 40960 rows of 2048 back, with an added gradient and the weight's, 671 MB, 109.5 us, 6.1 TB/s; forward with
-// a residual 112 us, 6.0; 8192 rows forward 24.5, 5.5, back 27.8 (4.3 of it the second launch); 262144 heads of 128 back 39.2, 5.1 (the same); 16 rows 3.4 on the GPU.
+// a residual 112 us, 6.0; 8192 rows forward 24.5, 5.5, back 27.8 (4.3 of it the second launch); 262144 heads of 128 back 38.7, 5.2 (the same); 16 rows 3.4 on the GPU.
 #include "moe_common.h"
 #include "pieces.h"
 
@@ -21,7 +21,7 @@ namespace {
 constexpr int kMaxDim = 16384;
 // 16-byte pieces of a row that one lane holds; of shorter rows, several at once.  Back, a lane's registers hold weights, two sums and the next row beside a row: with
 // four pieces 40960 rows of 2048 took 117 us, 110 with two, as layer norm with bias 189 (registers spilled), 111 with two.  Forward four are better: 8192 rows 24.5,
-// 25.1 with two.
+// 25.1 with two.  All in bf16; fp32, where two pieces are half the elements and registers, goes by the same numbers without measurements of its own.
 constexpr int kFwdPieces = 4, kBwdPieces = 2;
 constexpr int kFwdThreads = 256, kBwdThreads = 512, kMaxThreads = 1024;   // at least; a row of more waves has a workgroup of them
 // at most: forward 40960 rows with residual 116.9 us with 2048, 112.2 with 4096, 111.1 with 8192, without residual 58.1, 56.4 and 61.4; back 256 leave the fewest
@@ -408,7 +408,9 @@ void launch_bwd(const NormArgs& a, const RowSplit& s, int dtype, bool layer, int
       constexpr int N = decltype(n)::value, P = decltype(p)::value, U = rows_at_once(P, kBwdPieces), KIND = decltype(kind)::value;
       constexpr bool LAYER = KIND == 2, DB = KIND > 0, ADD = decltype(add)::value;
       if constexpr (P == kBwdPieces || (P > kBwdPieces && sizeof(E) == 4)) {
-        if (threads > kBwdThreads) {                   // more than 8192 elements (bf16; 4096 in fp32): 128 registers a lane, some kinds spill
+        if (threads > kBwdThreads) {                   // more than 8192 elements (bf16; 4096 in fp32): 128 registers a lane
+          // Above 8192 elements all kinds but one spill, 12 to 42 registers in bf16, 22 to 120 in fp32.  8192 rows of 16384 in bf16: rms 141 us (none; 5.7 TB/s), with an
+          // added gradient 210 (14 spilled; 5.1), layer norm with bias 185 (12), with both 363 (42; 3.0); 4096 rows in fp32 162, 426, 241 and 469 (22, 96, 49, 112)
           MOE_LAUNCH("norm_bwd", (norm_bwd_kernel<E, N, P, U, LAYER, DB, ADD, kMaxThreads>), dim3(blocks), dim3(threads), lds, st, a);
           return;
         }

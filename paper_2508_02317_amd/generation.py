@@ -6,7 +6,7 @@ transformer block over it.
 
 The projections are plain library products; rotation, cache and the attention of single tokens are calls into libmoe on the current
 stream; positions may have several axes.  Which pages a sequence has is decided here, on the host, and reaches the device as four small tensors per step and layer, each
-a copy that the host waits for.
+a copy that the host waits for; positions of several axes are a fifth, beside which those of one axis among the four go unused.
 """
 import math
 
